@@ -20,6 +20,8 @@
  * and decoder put around it, each documented at its declaration below: the hoisted product by itself (lstm_gemm),
  * max-pooling in time between encoder layers (lstm_time_pool_fwd / _bwd), one step of the attention decoder
  * (lstm_attention_step, lstm_readout), one step of batched beam search (lstm_beam_step, lstm_beam_gather, lstm_beam_gather_many, lstm_embed),
+ * what the training of a recurrent language model has around its layers (lstm_gated_scan_fwd / _bwd, a recurrence without a product per
+ * step; lstm_label_score_fwd / _bwd, log probabilities of labels with their gradient; lstm_grad_norm and lstm_adamw_step),
  * and diagnostics (lstm_sync_status, lstm_profile_*, lstm_strerror).
  *
  * Conventions common to every entry point
@@ -293,6 +295,113 @@ int lstm_beam_step_static(int Q, int beam, int V, const float* logits, int64_t l
                           int32_t* src, int32_t* label, void* stream);
 int lstm_embed(int B, int n, int V, const int32_t* label, const void* W_trg, const float* b_trg, void* out,
                int64_t ld_out, void* stream);
+
+/* A gated linear recurrence over time: a recurrent layer whose gates do not see the previous state, so that no matrix product is left
+ * inside the loop.  From pre-activations z = x W + b for all frames (one lstm_gemm, as for the LSTM layer; 3n columns, gate blocks f | g | o):
+ *     f, o = sigmoid(z_f, z_o)    g = tanh(z_g)    c_t = f * c_{t-1} + (1 - f) * g    y_t = o * c_t
+ * Masks, directions and state are the layer's: frame t of row b is valid iff t < seq_lens[b] (NULL: all T); at a padded frame the state is
+ * carried, y and dz are 0, and what z and dy hold there never reaches a result; direction -1 walks t = T-1 .. 0.  T == 1 is the step of
+ * a search or of generation: feed cT back as c0.
+ *   dtype: LSTM_F32 or LSTM_BF16_F32STATE, the type of z, y, dy, dz; states, dc0, dcT, db are float, and so is all arithmetic.
+ *   z [T][B][ldz >= 3n]  y [T][B][ldy >= n] (e.g. one half of a wider row)  c0, cT [B][n]: c0 may be NULL (zeros), cT NULL (not wanted) or c0.
+ *   reserve: reserve_bytes of lstm_gated_scan_query, written by the forward call for the backward call (the state before every 16th
+ *   valid frame, from which the backward call works the others out again); NULL: no backward call follows.
+ * Backward: the exact gradient of sum(dy*y) + sum(dcT*cT), from the forward call's z, seq_lens and reserve, and the same T, B, n, direction.
+ *   dy [T][B][lddy >= n]  dcT [B][n] or NULL (zeros)
+ *   -> dz [T][B][lddz >= 3n]; dc0 [B][n] or NULL (not wanted); db [3n], the sum of dz over all valid frames before its rounding, or NULL.
+ * The gradients of x and W are products of dz (lstm_gemm, with seq_lens masking the frames).  Rows may start at any element; whole words of
+ * two bfloat16 values (even n, ld and addresses of whole words) are faster.  T == 0 or B == 0 is legal: cT = c0, dc0 = dcT, db = 0.
+ * Only cT may overlap an input (c0).  workspace: workspace_bytes of the query, for either call; nothing in it has to survive a call.
+ * Calls with the same inputs agree bit for bit.
+ * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative T or B, n < 1, ld too small, more than 2^31 - 1 rows or states), LSTM_ERR_DIRECTION, LSTM_ERR_UNSUPPORTED
+ * (dtype), LSTM_ERR_ALIGN (element alignment), LSTM_ERR_SIZE (reserve or workspace), LSTM_ERR_HIP. */
+int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* workspace_bytes);
+int lstm_gated_scan_fwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const float* c0, const int32_t* seq_lens,
+                        void* y, int64_t ldy, float* cT, void* reserve, uint64_t reserve_bytes, void* workspace, uint64_t workspace_bytes,
+                        void* stream);
+int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const int32_t* seq_lens, const void* reserve,
+                        uint64_t reserve_bytes, const void* dy, int64_t lddy, const float* dcT, void* dz, int64_t lddz, float* dc0, float* db,
+                        void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Log probabilities of given labels under the softmax of an output layer's logits, the entropy of every row's distribution and its best
+ * labels, and the gradient: the loss of a training step, and the scoring of given text.  With x = logits of row (t, b):
+ *     m = max_v x[v]    log z = log sum_v exp(x[v] - m)    logp = (x[label] - m) - log z    log p = (x - m) - log z    entropy = -sum_v p[v] log p[v]
+ *     top_logp[k], top_label[k]: the `top` largest log p[v], best first, equal ones by the smaller v
+ *     dlogits[v] = dlogp * ([v = label] - p[v]) - dent * p[v] * (log p[v] + entropy)
+ *   A row is valid iff t < seq_lens[b] (NULL: all); a padded row gives logp = entropy = m = log z = 0, no alternatives, dlogits = 0, and its
+ *   logits, label and gradients are not used.  Rows without time: T = 1, seq_lens NULL.
+ *   A label outside [0, V) stands for "none": logp = 0, and dlogp of that row is not used.  A logit of -inf is a label that cannot occur: p = 0, no alternative,
+ *   gradient 0.  Where nothing can occur (all -inf): m = -inf, log z = 0, logp = -inf, entropy = 0, gradient 0.  A NaN or +inf among a row's
+ *   logits makes its values and its gradient NaN, and it has no alternatives.  Places without an alternative hold -inf and label 0.
+ *   Where dlogp and dent of a row are both 0 (or not given) its gradient is 0 and its logits are not read.
+ *   dtype: LSTM_F32 or LSTM_BF16_F32STATE, the type of logits and dlogits; all else is float or int32, all arithmetic float, the values before
+ *   their rounding for dlogits.
+ *   logits [T][B][ld >= V]  label int32 [T][B]  logp, entropy float [T][B]  stats float [T][B][2]: m and log z (their sum is the
+ *   log of the sum of exponentials; apart they keep their digits whatever the size of the logits)  top_logp float, top_label int32 [T][B][top], 0 <= top <= 16
+ *   Forward: label and logp may both be NULL, entropy and stats may be; top_logp and top_label may be NULL with top = 0 only.
+ *   Backward: stats (and entropy, with dent) from the forward call; dlogp, dent float [T][B] or NULL (zeros); label may be NULL without dlogp;
+ *   dlogits [T][B][ldd >= V], which may be logits (with ldd = ld).
+ *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call); nothing in it has to survive a call.
+ * Calls with the same inputs agree bit for bit.
+ * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0), LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN,
+ * LSTM_ERR_SIZE, LSTM_ERR_HIP. */
+int lstm_label_score_query(int T, int B, int V, int top, uint64_t* workspace_bytes);
+int lstm_label_score_fwd(int dtype, int T, int B, int V, const void* logits, int64_t ld, const int32_t* label, const int32_t* seq_lens,
+                         float* logp, float* entropy, float* stats, int top, float* top_logp, int32_t* top_label, void* workspace,
+                         uint64_t workspace_bytes, void* stream);
+int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int64_t ld, const int32_t* label, const int32_t* seq_lens,
+                         const float* stats, const float* entropy, const float* dlogp, const float* dent, void* dlogits, int64_t ldd, void* stream);
+
+/* The update of a model's weights from the gradients that the backward calls leave: AdamW over any number of tensors at once, and the
+ * global norm of the gradients that it is clipped by.  `items` is a HOST array, read during the call.
+ *
+ * lstm_grad_norm: out[0] = sqrt(sum over all tensors of grad^2), summed in 64 bits in a fixed order; out[1] = min(1, max_norm / out[0]), the factor
+ *   that clips it to max_norm, or NaN if the norm is not finite.  Only grad, grad_dtype and count of the items are read.
+ *   max_norm > 0 (infinity: never clipped).  out: float [2] in device memory; workspace of lstm_grad_norm_query bytes.
+ *
+ * lstm_adamw_step: with g = grad * grad_scale (*grad_scale in device memory, e.g. out + 1 of lstm_grad_norm; NULL: 1) and t the number of this step, from 1,
+ *     m = beta1 m + (1 - beta1) g    v = beta2 v + (1 - beta2) g^2
+ *     w = w (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ *   A grad_scale that is not finite leaves everything as it was: a step whose gradients overflowed is passed over without the host looking.
+ *   w is `master` where there is one, and `param` is its rounding; otherwise w is `param` itself.
+ *   States of LSTM_STATE_F32: m and v are float.  LSTM_STATE_8BIT: m and r = sqrt(v) lie in blocks of 256 elements (the last one of a tensor
+ *   may be short) as 8-bit floats of 4 exponent and 3 mantissa bits (e4m3, largest value 448) in units of a float scale per block,
+ *   the block's largest magnitude / 448: m[i] stands for m[i] * m_scale[i / 256], v[i] for (v[i] * v_scale[i / 256])^2.  w is updated with m and v
+ *   as computed, before their rounding (to nearest; a positive r never becomes 0, so no element's next step divides a remembered
+ *   gradient by nothing).  States of zeros (bytes and scales) are the start.  An infinite m or r makes its block of 256 NaN.
+ *   lr and step may be in device memory (lr_dev, step_dev: not NULL), so that a captured call follows a schedule; lr and step are then not read
+ *   (a step below 1 there counts as 1).
+ *   The same tensor must not occur twice, nor overlap another.  count may be 0 for a tensor (nothing done) and for the call.
+ *   Any element alignment is taken; tensors whose arrays start at multiples of 16 bytes (8-bit states: of 4, bfloat16: of 8) are faster.
+ * Both only enqueue work, allocate nothing and give the same bits for the same inputs.
+ * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative counts, step < 1, lr, beta, eps, max_norm out of range: lr, eps >= 0 and 0 <= beta < 1, finite),
+ * LSTM_ERR_UNSUPPORTED (dtypes, states, reserved not 0, a master of a float param), LSTM_ERR_ALIGN, LSTM_ERR_SIZE, LSTM_ERR_HIP. */
+typedef enum { LSTM_STATE_F32 = 0, LSTM_STATE_8BIT = 1 } lstm_state_dtype;
+typedef struct lstm_adamw_item {
+  void* param;                 /* device [count], updated */
+  float* master;               /* device [count] or NULL: the float weights behind a bfloat16 param, updated */
+  const void* grad;            /* device [count] */
+  void* m;                     /* device [count], updated, and so are the others below */
+  void* v;
+  float* m_scale;              /* LSTM_STATE_8BIT only: device [ceil(count / 256)] */
+  float* v_scale;
+  int64_t count;               /* elements */
+  int32_t param_dtype;         /* lstm_dtype: LSTM_F32 or LSTM_BF16_F32STATE */
+  int32_t grad_dtype;
+  float weight_decay;
+  int32_t reserved;            /* must be 0 */
+} lstm_adamw_item;
+typedef struct lstm_adamw_desc {
+  double lr, beta1, beta2, eps;
+  int32_t step;                /* t of the formula */
+  int32_t state_dtype;         /* lstm_state_dtype, for all items */
+  const float* lr_dev;
+  const int32_t* step_dev;
+  const float* grad_scale;
+} lstm_adamw_desc;
+int lstm_grad_norm_query(int count, const lstm_adamw_item* items, uint64_t* workspace_bytes);
+int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, float* out, void* workspace, uint64_t workspace_bytes, void* stream);
+int lstm_adamw_step(const lstm_adamw_desc* desc, int count, const lstm_adamw_item* items, void* stream);
 
 /* Diagnostic for the single-launch (persistent) recurrent kernels, whose work-groups wait for each
  * other between time steps with BOUNDED waits.  If a wait ever expired, the kernel drained early, the

@@ -17,7 +17,8 @@ LSTM_F32, LSTM_BF16_F32STATE = 0, 1
 FLAG_ACCUMULATE, FLAG_PER_STEP, FLAG_INFERENCE, FLAG_WEIGHTS_PACKED, FLAG_PLAIN_LAUNCH = 1, 2, 4, 8, 16
 EXPORTS = ("lstm_query", "lstm_fwd", "lstm_bwd", "blstm_fwd", "blstm_bwd", "lstm_gemm", "lstm_time_pool_fwd", "lstm_time_pool_bwd", "lstm_attention_query", "lstm_attention_step",
            "lstm_readout_query", "lstm_readout", "lstm_beam_query", "lstm_beam_step", "lstm_beam_step_static", "lstm_beam_gather", "lstm_beam_gather_many", "lstm_embed",
-           "lstm_sync_status", "lstm_profile_enable", "lstm_profile_read",
+           "lstm_gated_scan_query", "lstm_gated_scan_fwd", "lstm_gated_scan_bwd", "lstm_label_score_query", "lstm_label_score_fwd", "lstm_label_score_bwd",
+           "lstm_grad_norm_query", "lstm_grad_norm", "lstm_adamw_step", "lstm_sync_status", "lstm_profile_enable", "lstm_profile_read",
            "lstm_strerror")
 
 
@@ -35,6 +36,17 @@ class LstmDesc(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("B", ctypes.c_int32), ("n_in", ctypes.c_int32), ("n", ctypes.c_int32),
                 ("direction", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("reserve_bytes", ctypes.c_uint64), ("workspace_bytes", ctypes.c_uint64)]
+
+
+class AdamwItem(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("count", ctypes.c_int64), ("param_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("weight_decay", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int32),
+                ("state_dtype", ctypes.c_int32), ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
 
 
 class LstmError(RuntimeError):
@@ -87,6 +99,26 @@ def _load():
     lib.lstm_beam_gather_many.argtypes = [ip, ip, ip, ctypes.POINTER(GatherItem), vp, vp]
     lib.lstm_embed.restype = ip
     lib.lstm_embed.argtypes = [ip, ip, ip, vp, vp, vp, vp, i64, vp]
+    u64 = ctypes.c_uint64
+    lib.lstm_gated_scan_query.restype = ip
+    lib.lstm_gated_scan_query.argtypes = [ip, ip, ip, u64p, u64p]
+    lib.lstm_gated_scan_fwd.restype = ip
+    lib.lstm_gated_scan_fwd.argtypes = [ip] * 5 + [vp, i64, vp, vp, vp, i64, vp, vp, u64, vp, u64, vp]
+    lib.lstm_gated_scan_bwd.restype = ip
+    lib.lstm_gated_scan_bwd.argtypes = [ip] * 5 + [vp, i64, vp, vp, u64, vp, i64, vp, vp, i64, vp, vp, vp, u64, vp]
+    lib.lstm_label_score_query.restype = ip
+    lib.lstm_label_score_query.argtypes = [ip] * 4 + [u64p]
+    lib.lstm_label_score_fwd.restype = ip
+    lib.lstm_label_score_fwd.argtypes = [ip] * 4 + [vp, i64, vp, vp, vp, vp, vp, ip, vp, vp, vp, u64, vp]
+    lib.lstm_label_score_bwd.restype = ip
+    lib.lstm_label_score_bwd.argtypes = [ip] * 4 + [vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    itp = ctypes.POINTER(AdamwItem)
+    lib.lstm_grad_norm_query.restype = ip
+    lib.lstm_grad_norm_query.argtypes = [ip, itp, u64p]
+    lib.lstm_grad_norm.restype = ip
+    lib.lstm_grad_norm.argtypes = [ip, itp, ctypes.c_float, vp, vp, u64, vp]
+    lib.lstm_adamw_step.restype = ip
+    lib.lstm_adamw_step.argtypes = [ctypes.POINTER(AdamwDesc), ip, itp, vp]
     lib.lstm_sync_status.restype = ip
     lib.lstm_sync_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32)]
     lib.lstm_profile_enable.restype = ip
@@ -143,6 +175,10 @@ def query(desc, bidirectional):
 
 def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _device():
+    return torch._C._cuda_getDevice()
 
 
 def _dtype_of(x):
@@ -268,6 +304,67 @@ def beam_gather_many(states, src, outs=None):
 def embed(label, W_trg, b_trg=None, *, out=None):
     """trg = W_trg[label] + b_trg through lstm_embed; label int32 (any shape), W_trg [V, n] bfloat16 -> [label.numel(), n] bfloat16."""
     return _checked(_marshal.embed(label, W_trg, b_trg, out, _stream()))[1]
+
+
+def gated_scan_query(T, B, n):
+    """-> bytes of reserve and of workspace."""
+    r, w = ctypes.c_uint64(0), ctypes.c_uint64(0)
+    _check(lib.lstm_gated_scan_query(T, B, n, ctypes.byref(r), ctypes.byref(w)))
+    return r.value, w.value
+
+
+def gated_scan_fwd(z, c0=None, seq_lens=None, *, direction=1, save=True, want_state=True, out=None, workspace=None):
+    """Gated linear recurrence over z [T, B, 3n] (f | g | o pre-activations, float or bfloat16; a view with evenly spaced rows is fine) through
+    lstm_gated_scan_fwd.  c0 float [B, n]; save: keep what gated_scan_bwd needs; out: optional [T, B, n] view to write y into.
+    -> dict(y, cT, reserve, workspace, direction).  One step of a search is T = 1, save=False, with cT fed back as c0."""
+    _, y, cT, reserve, workspace = _checked(_marshal.gated_scan_fwd(z, c0, seq_lens, direction, save, want_state, out, workspace, _device(), _stream()))
+    return dict(y=y, cT=cT, reserve=reserve, workspace=workspace, direction=direction)
+
+
+def gated_scan_bwd(fwd, z, dy, seq_lens=None, dcT=None, *, want_dstate=True, want_db=True, out=None, workspace=None):
+    """Gradient of gated_scan_fwd, from its result: dict(dz [T, B, 3n], dc0 [B, n], db [3n])."""
+    _, dz, dc0, db = _checked(_marshal.gated_scan_bwd(z, seq_lens, fwd["reserve"], dy, dcT, fwd["direction"], want_dstate, want_db, out, workspace,
+                                                      _device(), _stream()))
+    return dict(dz=dz, dc0=dc0, db=db)
+
+
+def label_score_fwd(logits, label=None, seq_lens=None, *, top=0, want_entropy=True, workspace=None):
+    """Log probabilities of `label` (int32, one per row) under the softmax of logits [T, B, V] or [B, V] (float or bfloat16), the rows' entropies and
+    their `top` best labels, through lstm_label_score_fwd.  -> dict(logp, entropy, stats, top_logp, top_label, workspace); stats [..., 2]: the row's
+    maximum and the log of its sum of exponentials from there."""
+    _, logp, entropy, stats, top_logp, top_label, workspace = _checked(_marshal.label_score_fwd(
+        logits, label, seq_lens, top, want_entropy, workspace, _device(), _stream()))
+    return dict(logp=logp, entropy=entropy, stats=stats, top_logp=top_logp, top_label=top_label, workspace=workspace)
+
+
+def label_score_bwd(fwd, logits, label, dlogp, dent=None, seq_lens=None, *, out=None):
+    """Gradient of sum(dlogp * logp) + sum(dent * entropy) for logits, from label_score_fwd's result; out: optional tensor like logits, or logits itself."""
+    return _checked(_marshal.label_score_bwd(logits, label, seq_lens, fwd["stats"], fwd["entropy"] if dent is not None else None, dlogp, dent, out,
+                                             _device(), _stream()))[1]
+
+
+def grad_norm(grads, max_norm=float("inf"), *, out=None, workspace=None):
+    """-> float tensor [2]: the 2-norm over all gradients, and the factor that clips it to max_norm (NaN if the norm is not finite)."""
+    return _checked(_marshal.grad_norm(grads, max_norm, out, workspace, _device(), _stream()))[1]
+
+
+def adamw_step(params, grads, m, v, *, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, masters=None, m_scale=None, v_scale=None,
+               grad_scale=None):
+    """One AdamW step over sequences of tensors, in place, through lstm_adamw_step.  params float or bfloat16, masters: their float values behind
+    bfloat16 (None, or a sequence that may hold None); m, v float, or float8_e4m3fn with m_scale and v_scale [ceil(count / 256)] (adamw_state makes
+    either); weight_decay: a number or one per tensor; lr and step: numbers or tensors of one element (float, int32) on the GPU; grad_scale: a float
+    tensor of one element, e.g. grad_norm(...)[1:]; if it holds no finite value the step changes nothing."""
+    _check(_marshal.adamw_step(params, grads, m, v, masters, m_scale, v_scale, weight_decay, lr, beta1, beta2, eps, step, grad_scale, _device(), _stream()))
+
+
+def adamw_state(params, bits=32):
+    """States of adamw_step before the first step: dict(m, v), or with bits=8 dict(m, v, m_scale, v_scale)."""
+    if bits == 32:
+        return {k: [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in params] for k in ("m", "v")}
+    assert bits == 8, "states have 32 bits or 8"
+    state = {k: [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for p in params] for k in ("m", "v")}
+    state.update({k: [torch.zeros(-(-p.numel() // 256), dtype=torch.float32, device=p.device) for p in params] for k in ("m_scale", "v_scale")})
+    return state
 
 
 PHASES = ("prep", "gemm_zx", "loop_fwd", "loop_bwd", "gemm_dx", "gemm_dwx", "gemm_dwh", "db")

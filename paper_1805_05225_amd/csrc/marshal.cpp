@@ -35,6 +35,15 @@ struct Abi {
   decltype(&lstm_embed) embed;
   decltype(&lstm_time_pool_fwd) pool_fwd;
   decltype(&lstm_time_pool_bwd) pool_bwd;
+  decltype(&lstm_gated_scan_query) scan_query;
+  decltype(&lstm_gated_scan_fwd) scan_fwd;
+  decltype(&lstm_gated_scan_bwd) scan_bwd;
+  decltype(&lstm_label_score_query) score_query;
+  decltype(&lstm_label_score_fwd) score_fwd;
+  decltype(&lstm_label_score_bwd) score_bwd;
+  decltype(&lstm_grad_norm_query) norm_query;
+  decltype(&lstm_grad_norm) norm;
+  decltype(&lstm_adamw_step) adamw;
 } abi;
 
 struct Failed {};                                   // a Python exception is set
@@ -347,6 +356,279 @@ FAST(time_pool_bwd) {
   });
 }
 
+// A tensor of the scan, the score and the update: on the device that the call's stream belongs to, of the type that the entry point reads.
+const at::Tensor& placed(PyObject* o, long device, const char* what) {
+  const at::Tensor& t = tensor(o);
+  require(t.is_cuda() && t.get_device() == device, what);
+  return t;
+}
+constexpr const char* kWhere = "tensors lie on the current GPU";
+bool stored(const at::Tensor& t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+// optional contiguous tensor of a given type and number of elements
+template <typename T>
+T* whole(PyObject* o, long device, at::ScalarType type, int64_t count, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = placed(o, device, kWhere);
+  require(t.scalar_type() == type && t.numel() == count && t.is_contiguous(), what);
+  return (T*)t.data_ptr();
+}
+// Distance of the rows of [T, B, F] (or [B, F]) in elements: rows are contiguous and follow each other evenly.
+int64_t row_stride(const at::Tensor& t, const char* what) {
+  const int64_t d = t.dim(), F = t.size(d - 1), B = t.size(d - 2), T = d == 3 ? t.size(0) : 1;
+  if (t.numel() == 0) return F;
+  require(F == 1 || t.stride(d - 1) == 1, what);
+  const int64_t ld = B > 1 ? t.stride(d - 2) : T > 1 ? t.stride(0) : F;
+  require(T == 1 || t.stride(0) == B * ld, what);
+  return ld;
+}
+// workspace of `need` bytes: `o` if it is given (the library checks its size), otherwise a new one
+at::Tensor scratch_of(PyObject* o, const at::Tensor& like, uint64_t need, long device) {
+  if (o == Py_None) return bytes_like(like, (int64_t)need);
+  const at::Tensor& t = placed(o, device, kWhere);
+  require(t.is_contiguous() && t.scalar_type() == at::kByte, "a workspace is a contiguous tensor of bytes");
+  return t;
+}
+
+// z c0 lens | direction save want_state out workspace device stream  -> (status, y, cT, reserve, workspace)
+FAST(gated_scan_fwd) {
+  return guarded<10>(nargs, [&]() -> PyObject* {
+    const long dev = integer(a[8]);
+    const at::Tensor& z = placed(a[0], dev, kWhere);
+    require(z.dim() == 3 && z.size(2) % 3 == 0 && stored(z), "z is [T, B, 3n], float or bfloat16");
+    const int64_t T = z.size(0), B = z.size(1), n = z.size(2) / 3, ldz = row_stride(z, "rows of z are contiguous and evenly spaced");
+    uint64_t rb = 0, wb = 0;
+    int rc = T > INT32_MAX || B > INT32_MAX || n > INT32_MAX ? (int)LSTM_ERR_DIM : abi.scan_query((int)T, (int)B, (int)n, &rb, &wb);
+    if (rc) return Py_BuildValue("(i)", rc);
+    const float* c0 = whole<float>(a[1], dev, at::kFloat, B * n, "c0 is a contiguous float [B, n]");
+    const int32_t* lens = whole<int32_t>(a[2], dev, at::kInt, B, "seq_lens is a contiguous int32 [B]");
+    const at::Tensor y = a[6] != Py_None ? placed(a[6], dev, kWhere) : at::empty({T, B, n}, z.options());
+    require(y.dim() == 3 && y.size(0) == T && y.size(1) == B && y.size(2) == n && y.scalar_type() == z.scalar_type(), "out is [T, B, n] of z's type");
+    const int64_t ldy = row_stride(y, "rows of out are contiguous and evenly spaced");
+    at::Tensor cT, reserve;
+    if (truth(a[5])) cT = at::empty({B, n}, z.options().dtype(at::kFloat));
+    if (truth(a[4])) reserve = bytes_like(z, (int64_t)rb);
+    const at::Tensor ws = scratch_of(a[7], z, wb, dev);
+    rc = call(abi.scan_fwd, storage(z), (int)integer(a[3]), (int)T, (int)B, (int)n, z.data_ptr(), ldz, c0, lens, y.data_ptr(), ldy,
+              cT.defined() ? (float*)cT.data_ptr() : nullptr, reserve.defined() ? reserve.data_ptr() : nullptr, rb, ws.data_ptr(), (uint64_t)ws.numel(),
+              stream_of(a[9]));
+    return Py_BuildValue("(iNNNN)", rc, wrapped(y), wrapped(cT), wrapped(reserve), wrapped(ws));
+  });
+}
+
+// z lens reserve dy dcT | direction want_dstate want_db out workspace device stream  -> (status, dz, dc0, db)
+FAST(gated_scan_bwd) {
+  return guarded<12>(nargs, [&]() -> PyObject* {
+    const long dev = integer(a[10]);
+    const at::Tensor &z = placed(a[0], dev, kWhere), &reserve = placed(a[2], dev, kWhere), &dy = placed(a[3], dev, kWhere);
+    require(z.dim() == 3 && z.size(2) % 3 == 0 && stored(z), "z is [T, B, 3n], float or bfloat16");
+    const int64_t T = z.size(0), B = z.size(1), n = z.size(2) / 3, ldz = row_stride(z, "rows of z are contiguous and evenly spaced");
+    uint64_t rb = 0, wb = 0;
+    int rc = T > INT32_MAX || B > INT32_MAX || n > INT32_MAX ? (int)LSTM_ERR_DIM : abi.scan_query((int)T, (int)B, (int)n, &rb, &wb);
+    if (rc) return Py_BuildValue("(i)", rc);
+    require(dy.dim() == 3 && dy.size(0) == T && dy.size(1) == B && dy.size(2) == n && dy.scalar_type() == z.scalar_type(), "dy is [T, B, n] of z's type");
+    const int64_t lddy = row_stride(dy, "rows of dy are contiguous and evenly spaced");
+    const int32_t* lens = whole<int32_t>(a[1], dev, at::kInt, B, "seq_lens is a contiguous int32 [B]");
+    const float* dcT = whole<float>(a[4], dev, at::kFloat, B * n, "dcT is a contiguous float [B, n]");
+    require(reserve.is_contiguous() && reserve.scalar_type() == at::kByte, "reserve is the forward call's");
+    const at::Tensor dz = a[8] != Py_None ? placed(a[8], dev, kWhere) : at::empty({T, B, 3 * n}, z.options());
+    require(dz.dim() == 3 && dz.sizes() == z.sizes() && dz.scalar_type() == z.scalar_type(), "out is [T, B, 3n] of z's type");
+    const int64_t lddz = row_stride(dz, "rows of out are contiguous and evenly spaced");
+    const auto f32 = z.options().dtype(at::kFloat);
+    at::Tensor dc0, db;
+    if (truth(a[6])) dc0 = at::empty({B, n}, f32);
+    if (truth(a[7])) db = at::empty({3 * n}, f32);
+    const at::Tensor ws = scratch_of(a[9], z, wb, dev);
+    rc = call(abi.scan_bwd, storage(z), (int)integer(a[5]), (int)T, (int)B, (int)n, z.data_ptr(), ldz, lens, reserve.data_ptr(), (uint64_t)reserve.numel(),
+              dy.data_ptr(), lddy, dcT, dz.data_ptr(), lddz, dc0.defined() ? (float*)dc0.data_ptr() : nullptr, db.defined() ? (float*)db.data_ptr() : nullptr,
+              ws.data_ptr(), (uint64_t)ws.numel(), stream_of(a[11]));
+    return Py_BuildValue("(iNNN)", rc, wrapped(dz), wrapped(dc0), wrapped(db));
+  });
+}
+
+struct ScoreShape { int64_t T, B, V, ld; };
+ScoreShape score_shape(const at::Tensor& x) {
+  require((x.dim() == 2 || x.dim() == 3) && stored(x), "logits are [T, B, V] or [B, V], float or bfloat16");
+  const int64_t d = x.dim();
+  return {d == 3 ? x.size(0) : 1, x.size(d - 2), x.size(d - 1), row_stride(x, "rows of logits are contiguous and evenly spaced")};
+}
+
+// logits label lens | top want_entropy workspace device stream  -> (status, logp, entropy, stats, top_logp, top_label, workspace)
+FAST(label_score_fwd) {
+  return guarded<8>(nargs, [&]() -> PyObject* {
+    const long dev = integer(a[6]), top = integer(a[3]);
+    const at::Tensor& x = placed(a[0], dev, kWhere);
+    const ScoreShape s = score_shape(x);
+    uint64_t need = 0;
+    int rc = s.T > INT32_MAX || s.B > INT32_MAX || s.V > INT32_MAX || top != (int)top ? (int)LSTM_ERR_DIM : abi.score_query((int)s.T, (int)s.B, (int)s.V, (int)top, &need);
+    if (rc) return Py_BuildValue("(i)", rc);
+    const int32_t* label = whole<int32_t>(a[1], dev, at::kInt, s.T * s.B, "label is a contiguous int32 tensor, one for every row of logits");
+    const int32_t* lens = whole<int32_t>(a[2], dev, at::kInt, s.B, "seq_lens is a contiguous int32 [B]");
+    auto shape = x.sizes().vec();
+    shape.pop_back();
+    const auto f32 = x.options().dtype(at::kFloat);
+    at::Tensor logp, entropy, top_logp, top_label;
+    shape.push_back(2);
+    const at::Tensor stats = at::empty(shape, f32);
+    shape.pop_back();
+    if (a[1] != Py_None) logp = at::empty(shape, f32);
+    if (truth(a[4])) entropy = at::empty(shape, f32);
+    if (top > 0) {
+      shape.push_back(top);
+      top_logp = at::empty(shape, f32);
+      top_label = at::empty(shape, x.options().dtype(at::kInt));
+    }
+    const at::Tensor ws = scratch_of(a[5], x, need, dev);
+    const auto p = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    rc = call(abi.score_fwd, storage(x), (int)s.T, (int)s.B, (int)s.V, x.data_ptr(), s.ld, label, lens, (float*)p(logp), (float*)p(entropy), (float*)p(stats),
+              (int)top, (float*)p(top_logp), (int32_t*)p(top_label), ws.data_ptr(), (uint64_t)ws.numel(), stream_of(a[7]));
+    return Py_BuildValue("(iNNNNNN)", rc, wrapped(logp), wrapped(entropy), wrapped(stats), wrapped(top_logp), wrapped(top_label), wrapped(ws));
+  });
+}
+
+// logits label lens stats entropy dlogp dent | out device stream  -> (status, dlogits)
+FAST(label_score_bwd) {
+  return guarded<10>(nargs, [&]() -> PyObject* {
+    const long dev = integer(a[8]);
+    const at::Tensor& x = placed(a[0], dev, kWhere);
+    const ScoreShape s = score_shape(x);
+    if (s.T > INT32_MAX || s.B > INT32_MAX || s.V > INT32_MAX) return Py_BuildValue("(i)", (int)LSTM_ERR_DIM);
+    const int64_t rows = s.T * s.B;
+    const int32_t* label = whole<int32_t>(a[1], dev, at::kInt, rows, "label is a contiguous int32 tensor, one for every row of logits");
+    const int32_t* lens = whole<int32_t>(a[2], dev, at::kInt, s.B, "seq_lens is a contiguous int32 [B]");
+    const float* in[4];
+    for (int i = 0; i < 4; ++i) in[i] = whole<float>(a[3 + i], dev, at::kFloat, i == 0 ? 2 * rows : rows, "stats (two values), entropy, dlogp and dent (one) are contiguous float tensors for every row of logits");
+    const at::Tensor out = a[7] != Py_None ? placed(a[7], dev, kWhere) : at::empty(x.sizes(), x.options());
+    require(out.sizes() == x.sizes() && out.scalar_type() == x.scalar_type(), "out has the shape and type of logits");
+    const int64_t ldd = row_stride(out, "rows of out are contiguous and evenly spaced");
+    const int rc = call(abi.score_bwd, storage(x), (int)s.T, (int)s.B, (int)s.V, x.data_ptr(), s.ld, label, lens, in[0], in[1], in[2], in[3], out.data_ptr(), ldd,
+                        stream_of(a[9]));
+    return Py_BuildValue("(iN)", rc, wrapped(out));
+  });
+}
+
+// The tensors of an update, read from sequences (None: not given), held until the call has returned.
+struct Update {
+  std::vector<lstm_adamw_item> item;
+  std::vector<at::Tensor> held;
+  long device;
+  explicit Update(long dev) : device(dev) {}
+  const at::Tensor& at_index(PyObject* seq, Py_ssize_t i) {
+    struct Ref { PyObject* o; ~Ref() { Py_XDECREF(o); } } ref{PySequence_GetItem(seq, i)};
+    if (!ref.o) throw Failed();
+    held.push_back(placed(ref.o, device, kWhere));
+    require(held.back().is_contiguous(), "tensors crossing the ABI must be contiguous");
+    return held.back();
+  }
+  void grads(PyObject* seq) {
+    const Py_ssize_t count = PySequence_Size(seq);
+    if (count < 0) throw Failed();
+    item.resize(count);
+    held.reserve(7 * count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+      const at::Tensor& t = at_index(seq, i);
+      require(stored(t), "gradients are float or bfloat16");
+      item[i] = {};
+      item[i].grad = t.data_ptr();
+      item[i].count = t.numel();
+      item[i].grad_dtype = storage(t);
+    }
+  }
+  // the i-th of `seq`, of `type` and of `n` elements
+  void* array(PyObject* seq, Py_ssize_t i, at::ScalarType type, int64_t n, const char* what) {
+    const at::Tensor& t = at_index(seq, i);
+    require(t.scalar_type() == type && t.numel() == n, what);
+    return t.data_ptr();
+  }
+  bool given(PyObject* seq, const char* what) {
+    if (seq == Py_None) return false;
+    const Py_ssize_t n = PySequence_Size(seq);
+    if (n < 0) throw Failed();
+    require(n == (Py_ssize_t)item.size(), what);
+    return true;
+  }
+};
+
+// grads max_norm | out workspace device stream  -> (status, out)
+FAST(grad_norm) {
+  return guarded<6>(nargs, [&]() -> PyObject* {
+    const long dev = integer(a[4]);
+    Update u(dev);
+    u.grads(a[0]);
+    const double max_norm = PyFloat_AsDouble(a[1]);
+    if (max_norm == -1.0 && PyErr_Occurred()) throw Failed();
+    uint64_t need = 0;
+    int rc = abi.norm_query((int)u.item.size(), u.item.data(), &need);
+    if (rc) return Py_BuildValue("(i)", rc);
+    require(!u.held.empty() || a[2] != Py_None, "no gradients, and no tensor for the result");
+    const at::Tensor out = a[2] != Py_None ? placed(a[2], dev, kWhere) : at::empty({2}, u.held[0].options().dtype(at::kFloat));
+    require(out.scalar_type() == at::kFloat && out.numel() == 2 && out.is_contiguous(), "out is a contiguous float [2]");
+    const at::Tensor ws = scratch_of(a[3], out, need, dev);
+    rc = call(abi.norm, (int)u.item.size(), u.item.data(), (float)max_norm, (float*)out.data_ptr(), ws.data_ptr(), (uint64_t)ws.numel(), stream_of(a[5]));
+    return Py_BuildValue("(iN)", rc, wrapped(out));
+  });
+}
+
+// params grads m v masters m_scale v_scale | weight_decay (a number or a sequence) lr beta1 beta2 eps step grad_scale device stream  -> status
+FAST(adamw_step) {
+  return guarded<16>(nargs, [&]() -> PyObject* {
+    Update u(integer(a[14]));
+    u.grads(a[1]);
+    const auto number = [](PyObject* o) {
+      const double x = PyFloat_AsDouble(o);
+      if (x == -1.0 && PyErr_Occurred()) throw Failed();
+      return x;
+    };
+    constexpr const char* kEach = "one parameter, gradient, state (and master, scale, weight decay) for every tensor";
+    require(u.given(a[0], kEach) && u.given(a[2], kEach) && u.given(a[3], kEach), kEach);
+    const bool masters = u.given(a[4], kEach), scales = u.given(a[5], kEach);
+    require(scales == u.given(a[6], kEach), "m_scale and v_scale are given together");
+    const bool decays = PySequence_Check(a[7]) && !PyFloat_Check(a[7]) && u.given(a[7], kEach);
+    const double decay = decays ? 0.0 : number(a[7]);
+    lstm_adamw_desc d = {};
+    d.state_dtype = scales ? LSTM_STATE_8BIT : LSTM_STATE_F32;
+    const at::ScalarType kind = scales ? at::kFloat8_e4m3fn : at::kFloat;
+    constexpr const char* kState = "states are float, or float8_e4m3fn with scales, with as many elements as the gradient";
+    constexpr const char* kScale = "scales are float, one for every 256 elements of the tensor";
+    for (Py_ssize_t i = 0; i < (Py_ssize_t)u.item.size(); ++i) {
+      lstm_adamw_item& it = u.item[i];
+      const at::Tensor& p = u.at_index(a[0], i);
+      require(stored(p) && p.numel() == it.count, "parameters are float or bfloat16, with as many elements as the gradient");
+      it.param = p.data_ptr();
+      it.param_dtype = storage(p);
+      it.m = u.array(a[2], i, kind, it.count, kState);
+      it.v = u.array(a[3], i, kind, it.count, kState);
+      if (scales) {
+        it.m_scale = (float*)u.array(a[5], i, at::kFloat, (it.count + 255) / 256, kScale);
+        it.v_scale = (float*)u.array(a[6], i, at::kFloat, (it.count + 255) / 256, kScale);
+      }
+      if (masters) {
+        struct Ref { PyObject* o; ~Ref() { Py_XDECREF(o); } } ref{PySequence_GetItem(a[4], i)};
+        if (!ref.o) throw Failed();
+        if (ref.o != Py_None) it.master = (float*)u.array(a[4], i, at::kFloat, it.count, "masters are float (or None), with as many elements as the gradient");
+      }
+      if (decays) {
+        struct Ref { PyObject* o; ~Ref() { Py_XDECREF(o); } } ref{PySequence_GetItem(a[7], i)};
+        if (!ref.o) throw Failed();
+        it.weight_decay = (float)number(ref.o);
+      } else {
+        it.weight_decay = (float)decay;
+      }
+    }
+    if (THPVariable_Check(a[8])) d.lr_dev = whole<float>(a[8], u.device, at::kFloat, 1, "lr is a number or a float tensor of one element");
+    else d.lr = number(a[8]);
+    d.beta1 = number(a[9]); d.beta2 = number(a[10]); d.eps = number(a[11]);
+    if (THPVariable_Check(a[12])) {
+      d.step_dev = whole<int32_t>(a[12], u.device, at::kInt, 1, "step is a number or an int32 tensor of one element");
+    } else {
+      const long t = integer(a[12]);
+      if (t > INT32_MAX || t < 1) return PyLong_FromLong(LSTM_ERR_DIM);
+      d.step = (int32_t)t;
+    }
+    d.grad_scale = whole<float>(a[13], u.device, at::kFloat, 1, "grad_scale is a float tensor of one element");
+    return PyLong_FromLong(call(abi.adamw, &d, (int)u.item.size(), u.item.data(), stream_of(a[15])));
+  });
+}
+
 // dict: entry point name -> address
 PyObject* bind(PyObject*, PyObject* table) {
   const auto at_name = [&](const char* name) -> void* {
@@ -358,7 +640,10 @@ PyObject* bind(PyObject*, PyObject* table) {
       {(void**)&abi.bbwd, "blstm_bwd"}, {(void**)&abi.gemm, "lstm_gemm"}, {(void**)&abi.att_query, "lstm_attention_query"},
       {(void**)&abi.att_step, "lstm_attention_step"}, {(void**)&abi.ro_query, "lstm_readout_query"}, {(void**)&abi.ro, "lstm_readout"},
       {(void**)&abi.beam_query, "lstm_beam_query"}, {(void**)&abi.beam, "lstm_beam_step"}, {(void**)&abi.gather_many, "lstm_beam_gather_many"},
-      {(void**)&abi.embed, "lstm_embed"}, {(void**)&abi.pool_fwd, "lstm_time_pool_fwd"}, {(void**)&abi.pool_bwd, "lstm_time_pool_bwd"}};
+      {(void**)&abi.embed, "lstm_embed"}, {(void**)&abi.pool_fwd, "lstm_time_pool_fwd"}, {(void**)&abi.pool_bwd, "lstm_time_pool_bwd"},
+      {(void**)&abi.scan_query, "lstm_gated_scan_query"}, {(void**)&abi.scan_fwd, "lstm_gated_scan_fwd"}, {(void**)&abi.scan_bwd, "lstm_gated_scan_bwd"},
+      {(void**)&abi.score_query, "lstm_label_score_query"}, {(void**)&abi.score_fwd, "lstm_label_score_fwd"}, {(void**)&abi.score_bwd, "lstm_label_score_bwd"},
+      {(void**)&abi.norm_query, "lstm_grad_norm_query"}, {(void**)&abi.norm, "lstm_grad_norm"}, {(void**)&abi.adamw, "lstm_adamw_step"}};
   for (auto& w : want) {
     *w.slot = at_name(w.name);
     if (!*w.slot) {
@@ -371,7 +656,8 @@ PyObject* bind(PyObject*, PyObject* table) {
 
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, ENTRY(forward), ENTRY(backward), ENTRY(gemm), ENTRY(attention_step), ENTRY(readout),
-                         ENTRY(beam_step), ENTRY(gather_many), ENTRY(embed), ENTRY(time_pool_fwd), ENTRY(time_pool_bwd), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(beam_step), ENTRY(gather_many), ENTRY(embed), ENTRY(time_pool_fwd), ENTRY(time_pool_bwd),
+                         ENTRY(gated_scan_fwd), ENTRY(gated_scan_bwd), ENTRY(label_score_fwd), ENTRY(label_score_bwd), ENTRY(grad_norm), ENTRY(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
