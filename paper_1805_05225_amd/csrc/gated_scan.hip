@@ -18,37 +18,38 @@ namespace {
 
 constexpr int kSeg = 16;              // valid frames between two kept states
 
-// A lane's access: V values of type T in one word.
+// A lane's access: V values of type T in one word, `at` elements behind a row that is the same for the whole wavefront.
 template <typename T, int V> struct Word;
 template <> struct Word<float, 1> {
-  static __device__ unsigned load(const void* p, long i) { return ((const unsigned*)p)[i]; }
+  static __device__ unsigned load(const void* p, unsigned at) { return ((const unsigned*)p)[at]; }
   static __device__ float get(unsigned w, int) { return __uint_as_float(w); }
-  static __device__ void store(void* p, long i, const float* v) { ((float*)p)[i] = v[0]; }
+  static __device__ void store(void* p, unsigned at, const float* v) { ((float*)p)[at] = v[0]; }
 };
 template <> struct Word<bf16_t, 1> {
-  static __device__ unsigned load(const void* p, long i) { return (unsigned)((const uint16_t*)p)[i] << 16; }
+  static __device__ unsigned load(const void* p, unsigned at) { return (unsigned)((const uint16_t*)p)[at] << 16; }
   static __device__ float get(unsigned w, int) { return __uint_as_float(w); }
-  static __device__ void store(void* p, long i, const float* v) { ((uint16_t*)p)[i] = f2bf_bits(v[0]); }
+  static __device__ void store(void* p, unsigned at, const float* v) { ((bf16_t*)p)[at] = (bf16_t)v[0]; }
 };
 template <> struct Word<bf16_t, 2> {
-  static __device__ unsigned load(const void* p, long i) { return *(const unsigned*)((const uint16_t*)p + i); }
+  typedef __attribute__((ext_vector_type(2))) float f2;
+  typedef __attribute__((ext_vector_type(2))) bf16_t b2;
+  static __device__ unsigned load(const void* p, unsigned at) { return *(const unsigned*)((const uint16_t*)p + at); }
   static __device__ float get(unsigned w, int k) { return __uint_as_float(k == 0 ? w << 16 : w & 0xffff0000u); }
-  static __device__ void store(void* p, long i, const float* v) {
-    *(unsigned*)((uint16_t*)p + i) = (unsigned)f2bf_bits(v[0]) | ((unsigned)f2bf_bits(v[1]) << 16);
+  static __device__ void store(void* p, unsigned at, const float* v) {
+    const f2 x = {v[0], v[1]};
+    *(b2*)((bf16_t*)p + at) = __builtin_convertvector(x, b2);    // rounded to nearest, ties to even
   }
 };
 
-// sigmoid(x) and 1 - sigmoid(x), each with the relative accuracy of a float (a forget gate near 1 leaves 1 - f its few bits otherwise)
+// sigmoid(x) and 1 - sigmoid(x) with e = exp(-x): 1 / (1 + e) and e / (1 + e), each with a float's relative accuracy (1 - f has few bits left
+// where a forget gate is near 1).  Where e is infinite the second is inf * 0 and becomes 1; a NaN stays in the first.
 __device__ __forceinline__ void sigmoid_pair(float x, float& s, float& not_s) {
-  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(x)), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-  s = x < 0.f ? small : big;                                    // (NaN: both are)
-  not_s = x < 0.f ? big : small;
+  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * x);
+  s = __builtin_amdgcn_rcpf(1.f + e);
+  not_s = fminf(e * s, 1.f);
 }
 __device__ __forceinline__ float sigmoid_(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x)); }
-__device__ __forceinline__ float tanh_(float x) {
-  const float e = __builtin_amdgcn_exp2f(-2.8853900817779268f * fabsf(x));
-  return copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x);
-}
+__device__ __forceinline__ float tanh_(float x) { return fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.8853900817779268f * x)), 1.f); }
 
 struct ScanArgs {
   const void* z; long ldz;
@@ -60,120 +61,368 @@ struct ScanArgs {
   const float* dcT;
   void* dz; long lddz;
   float* dc0;
-  float* dbpart;                      // [B][3n]
+  double* dbpart;                     // [parts * B][3n]
+  float2* join;                       // [parts][B][n]: what a part's frames do to a state, (factor, addend)
+  float* first;                       // [B][n]: copy of c0 or dcT
   int T, B, n, direction;
+  int parts, per;                     // time is cut into parts of `per` valid frames (a multiple of a work-group's round)
 };
 __device__ __forceinline__ int valid_frames(const int* lens, int b, int T) {
   if (!lens) return T;
-  const int L = lens[b];
+  const int L = __builtin_amdgcn_readfirstlane(lens[b]);
   return L < 0 ? 0 : (L > T ? T : L);
 }
+// The valid frames of a part, as numbers in the order of the walk, and where their rows lie.
+struct Span {
+  int L, begin, end;
+  long row0; int step;                // row of walk number i: row0 + i * step
+  __device__ __forceinline__ Span(const ScanArgs& a, int b, int part) {
+    L = valid_frames(a.lens, b, a.T);
+    begin = part * a.per;
+    end = min(L, begin + a.per);
+    row0 = a.direction > 0 ? b : (long)(L - 1) * a.B + b;
+    step = a.direction > 0 ? a.B : -a.B;
+  }
+};
+template <typename T> __device__ __forceinline__ const T* row_of(const void* p, long row, long ld) { return (const T*)p + row * ld; }
 
-// A lane walks V units of one row of the batch through time.
-template <typename T, int V>
-__global__ __launch_bounds__(64) void gated_scan_fwd_kernel(ScanArgs a) {
+// What a work-group's wavefronts tell each other: the composition of their frames, c -> A c + C, for every unit; two sets, so that one
+// barrier a round is enough.
+template <int V, int NW> struct Chain { float a[2][NW][V][64], c[2][NW][V][64]; };
+
+// The state that enters wavefront `wave`'s frames and the one that leaves all of them, from `state` and the NW compositions.  order: 1 if
+// wavefront 0 comes first, -1 if it comes last.
+template <int V, int NW>
+__device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wave, int order, const float (&A)[V], const float (&C)[V],
+                                     float (&state)[V], float (&mine)[V]) {
+  if constexpr (NW == 1) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) { mine[k] = state[k]; state[k] = fmaf(A[k], state[k], C[k]); }
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k) { s.a[set][wave][k][lane] = A[k]; s.c[set][wave][k][lane] = C[k]; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const int w = order > 0 ? i : NW - 1 - i;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        if (w == wave) mine[k] = state[k];
+        state[k] = fmaf(s.a[set][w][k][lane], state[k], s.c[set][w][k][lane]);
+      }
+    }
+  }
+}
+
+// A work-group takes 64 V units of one row of the batch through a part of time, NW * SEG frames a round: every wavefront has SEG of them in
+// registers, composes them into one step c -> A c + C, gets the state that enters them from the others' compositions and walks them
+// with it.  So all loads of a round are in flight together, z is read once and only the compositions cross wavefronts.
+template <typename T, int V, int NW, int SEG>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
-  const int b = blockIdx.y, u = (blockIdx.x * 64 + threadIdx.x) * V;
-  if (u >= a.n) return;
-  const int L = valid_frames(a.lens, b, a.T);
+  __shared__ Chain<V, NW> chain;
+  const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = (blockIdx.x * 64 + lane) * V;
+  const bool live = u < a.n;
+  const unsigned at = live ? u : 0;
+  const Span sp(a, b, part);
+  const float* c0 = a.parts > 1 ? a.first : a.c0;
   float c[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) c[k] = a.c0 ? a.c0[(long)b * a.n + u + k] : 0.f;
-  for (int i = 0; i < L; ++i) {
-    const int t = a.direction > 0 ? i : L - 1 - i;
-    if (a.kept && i % kSeg == 0) {
+  for (int k = 0; k < V; ++k) c[k] = c0 ? c0[(long)b * a.n + at + k] : 0.f;
+  if (sp.begin < sp.L)
+    for (int p = 0; p < part; ++p)
 #pragma unroll
-      for (int k = 0; k < V; ++k) a.kept[((long)(i / kSeg) * a.B + b) * a.n + u + k] = c[k];
-    }
-    const long row = (long)t * a.B + b;
-    const unsigned zf = W::load(a.z, row * a.ldz + u), zg = W::load(a.z, row * a.ldz + a.n + u), zo = W::load(a.z, row * a.ldz + 2L * a.n + u);
-    float y[V];
+      for (int k = 0; k < V; ++k) {
+        const float2 j = a.join[((long)p * a.B + b) * a.n + at + k];
+        c[k] = fmaf(j.x, c[k], j.y);
+      }
+  int set = 0;
+  for (int base = sp.begin; base < sp.end; base += NW * SEG, set ^= 1) {
+    const int s0 = base + wave * SEG, count = min(SEG, sp.end - s0);
+    float f[SEG][V], add[SEG][V], A[V], C[V], mine[V];
+    unsigned zo[SEG];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      float f, nf;
-      sigmoid_pair(W::get(zf, k), f, nf);
-      c[k] = fmaf(f, c[k], nf * tanh_(W::get(zg, k)));
-      y[k] = sigmoid_(W::get(zo, k)) * c[k];
+    for (int k = 0; k < V; ++k) { A[k] = 1.f; C[k] = 0.f; }
+    if (count > 0) {
+      unsigned zf[SEG], zg[SEG];
+#pragma unroll
+      for (int j = 0; j < SEG; ++j) {
+        const T* row = row_of<T>(a.z, sp.row0 + (long)(s0 + min(j, count - 1)) * sp.step, a.ldz);
+        zf[j] = W::load(row, at);
+        zg[j] = W::load(row + a.n, at);
+        zo[j] = W::load(row + 2L * a.n, at);
+      }
+#pragma unroll
+      for (int j = 0; j < SEG; ++j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          float nf;
+          sigmoid_pair(W::get(zf[j], k), f[j][k], nf);
+          add[j][k] = nf * tanh_(W::get(zg[j], k));
+          if (j >= count) { f[j][k] = 1.f; add[j][k] = 0.f; }
+          A[k] *= f[j][k];
+          C[k] = fmaf(f[j][k], C[k], add[j][k]);
+        }
     }
-    W::store(a.y, row * a.ldy + u, y);
+    link<V, NW>(chain, set, lane, wave, 1, A, C, c, mine);
+    if (count > 0) {
+      if (a.kept && live) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) a.kept[((long)(s0 / kSeg) * a.B + b) * a.n + u + k] = mine[k];
+      }
+#pragma unroll
+      for (int j = 0; j < SEG; ++j) {
+        float y[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          mine[k] = fmaf(f[j][k], mine[k], add[j][k]);
+          y[k] = sigmoid_(W::get(zo[j], k)) * mine[k];
+        }
+        if (live && j < count) W::store((T*)a.y + (sp.row0 + (long)(s0 + j) * sp.step) * a.ldy, at, y);
+      }
+    }
   }
+  if (!live) return;
   float zero[V] = {};
-  for (int t = L; t < a.T; ++t) W::store(a.y, ((long)t * a.B + b) * a.ldy + u, zero);
-  if (a.cT) {
+  for (int t = sp.L + part * NW + wave; t < a.T; t += a.parts * NW) W::store((T*)a.y + ((long)t * a.B + b) * a.ldy, at, zero);
+  if (a.cT && wave == 0 && (sp.L == 0 ? part == 0 : (sp.L - 1) / a.per == part)) {
 #pragma unroll
     for (int k = 0; k < V; ++k) a.cT[(long)b * a.n + u + k] = c[k];
   }
 }
 
-template <typename T, int V>
-__global__ __launch_bounds__(64) void gated_scan_bwd_kernel(ScanArgs a) {
+// The compositions of all parts but the last, for the kernel above, and a copy of c0 (which cT may overwrite while other parts read it).
+template <typename T, int V, int NW, int SEG>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
-  const int b = blockIdx.y, u = (blockIdx.x * 64 + threadIdx.x) * V;
-  if (u >= a.n) return;
-  const int L = valid_frames(a.lens, b, a.T);
-  float e[V], sum[3][V] = {};
+  __shared__ Chain<V, NW> chain;
+  const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = (blockIdx.x * 64 + lane) * V;
+  const bool live = u < a.n;
+  const unsigned at = live ? u : 0;
+  const Span sp(a, b, part);
+  if (part == 0 && live && wave == 0) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) e[k] = a.dcT ? a.dcT[(long)b * a.n + u + k] : 0.f;
-  for (int q = (L + kSeg - 1) / kSeg - 1; q >= 0; --q) {
-    float before[kSeg][V], c[V];
+    for (int k = 0; k < V; ++k) a.first[(long)b * a.n + u + k] = a.c0 ? a.c0[(long)b * a.n + u + k] : 0.f;
+  }
+  float A[V], C[V];
 #pragma unroll
-    for (int k = 0; k < V; ++k) c[k] = a.kept[((long)q * a.B + b) * a.n + u + k];
+  for (int k = 0; k < V; ++k) { A[k] = 1.f; C[k] = 0.f; }
+  for (int base = sp.begin; base < sp.end; base += NW * SEG) {
+    // each wavefront composes consecutive frames of its own eighth of the part
+    const int eighth = a.per / NW, from = sp.begin + wave * eighth, s0 = from + (base - sp.begin) / NW, count = min(SEG, min(sp.end, from + eighth) - s0);
+    if (count <= 0) break;
+    unsigned zf[SEG], zg[SEG];
 #pragma unroll
-    for (int j = 0; j < kSeg; ++j) {
-      const int i = min(q * kSeg + j, L - 1), t = a.direction > 0 ? i : L - 1 - i;
-      const long at = ((long)t * a.B + b) * a.ldz + u;
-      const unsigned zf = W::load(a.z, at), zg = W::load(a.z, at + a.n);
+    for (int j = 0; j < SEG; ++j) {
+      const T* row = row_of<T>(a.z, sp.row0 + (long)(s0 + min(j, count - 1)) * sp.step, a.ldz);
+      zf[j] = W::load(row, at);
+      zg[j] = W::load(row + a.n, at);
+    }
+#pragma unroll
+    for (int j = 0; j < SEG; ++j)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         float f, nf;
-        sigmoid_pair(W::get(zf, k), f, nf);
-        before[j][k] = c[k];
-        c[k] = fmaf(f, c[k], nf * tanh_(W::get(zg, k)));
+        sigmoid_pair(W::get(zf[j], k), f, nf);
+        float add = nf * tanh_(W::get(zg[j], k));
+        if (j >= count) { f = 1.f; add = 0.f; }
+        A[k] *= f;
+        C[k] = fmaf(f, C[k], add);
       }
-    }
-#pragma unroll
-    for (int j = kSeg - 1; j >= 0; --j) {
-      const int i = q * kSeg + j, t = a.direction > 0 ? i : L - 1 - i;
-      if (i < L) {
-        const long row = (long)t * a.B + b, at = row * a.ldz + u, to = row * a.lddz + u;
-        const unsigned zf = W::load(a.z, at), zg = W::load(a.z, at + a.n), zo = W::load(a.z, at + 2L * a.n), wy = W::load(a.dy, row * a.lddy + u);
-        float df[V], dg[V], dout[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          float f, nf, o, no;
-          sigmoid_pair(W::get(zf, k), f, nf);
-          sigmoid_pair(W::get(zo, k), o, no);
-          const float g = tanh_(W::get(zg, k)), dy = W::get(wy, k), now = fmaf(f, before[j][k], nf * g), dc = fmaf(dy, o, e[k]);
-          df[k] = dc * (before[j][k] - g) * f * nf;
-          dg[k] = dc * nf * fmaf(-g, g, 1.f);
-          dout[k] = dy * now * o * no;
-          e[k] = f * dc;
-          sum[0][k] += df[k]; sum[1][k] += dg[k]; sum[2][k] += dout[k];
-        }
-        W::store(a.dz, to, df);
-        W::store(a.dz, to + a.n, dg);
-        W::store(a.dz, to + 2L * a.n, dout);
-      }
-    }
   }
-  float zero[V] = {};
-  for (int t = L; t < a.T; ++t)
-    for (int gate = 0; gate < 3; ++gate) W::store(a.dz, ((long)t * a.B + b) * a.lddz + (long)gate * a.n + u, zero);
+#pragma unroll
+  for (int k = 0; k < V; ++k) { chain.a[0][wave][k][lane] = A[k]; chain.c[0][wave][k][lane] = C[k]; }
+  __syncthreads();
+  if (wave != 0 || !live) return;
 #pragma unroll
   for (int k = 0; k < V; ++k) {
-    if (a.dc0) a.dc0[(long)b * a.n + u + k] = e[k];
-    if (a.dbpart)
-      for (int gate = 0; gate < 3; ++gate) a.dbpart[((long)b * 3 + gate) * a.n + u + k] = sum[gate][k];
+    float2 j = make_float2(1.f, 0.f);
+    for (int w = 0; w < NW; ++w) {
+      j.x *= chain.a[0][w][k][lane];
+      j.y = fmaf(chain.a[0][w][k][lane], j.y, chain.c[0][w][k][lane]);
+    }
+    a.join[((long)part * a.B + b) * a.n + u + k] = j;
   }
 }
 
-// db = the sum of B rows of partial sums
-__global__ void scan_db_kernel(const float* __restrict__ part, float* __restrict__ db, int B, int n3) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
+// The same from the other end.  A wavefront works its SEG states out again from the one that the forward pass kept in front of them; what
+// passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.
+template <typename T, int V, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kernel(ScanArgs a) {
+  typedef Word<T, V> W;
+  constexpr int SEG = kSeg;
+  __shared__ union { Chain<V, NW> chain; double sum[NW][3][V][64]; } sh;
+  const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = (blockIdx.x * 64 + lane) * V;
+  const bool live = u < a.n;
+  const unsigned at = live ? u : 0;
+  const Span sp(a, b, part);
+  float e[V];
+  double total[3][V] = {};
+#pragma unroll
+  for (int k = 0; k < V; ++k) e[k] = a.dcT ? a.dcT[(long)b * a.n + at + k] : 0.f;
+  if (sp.begin < sp.L)
+    for (int p = (sp.L - 1) / a.per; p > part; --p)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float2 j = a.join[((long)p * a.B + b) * a.n + at + k];
+        e[k] = fmaf(j.x, e[k], j.y);
+      }
+  int set = 0;
+  for (int round = (sp.end - sp.begin + NW * SEG - 1) / (NW * SEG) - 1; round >= 0; --round, set ^= 1) {
+    const int s0 = sp.begin + (round * NW + wave) * SEG, count = min(SEG, sp.end - s0);
+    float f[SEG][V], nf[SEG][V], g[SEG][V], o[SEG][V], before[SEG][V], A[V], C[V], mine[V];
+    unsigned wy[SEG];
+#pragma unroll
+    for (int k = 0; k < V; ++k) { A[k] = 1.f; C[k] = 0.f; }
+    if (count > 0) {
+      unsigned zf[SEG], zg[SEG], zo[SEG];
+      float c[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) c[k] = a.kept[((long)(s0 / kSeg) * a.B + b) * a.n + at + k];
+#pragma unroll
+      for (int j = 0; j < SEG; ++j) {
+        const long r = sp.row0 + (long)(s0 + min(j, count - 1)) * sp.step;
+        const T* row = row_of<T>(a.z, r, a.ldz);
+        zf[j] = W::load(row, at);
+        zg[j] = W::load(row + a.n, at);
+        zo[j] = W::load(row + 2L * a.n, at);
+        wy[j] = W::load(row_of<T>(a.dy, r, a.lddy), at);
+      }
+#pragma unroll
+      for (int j = 0; j < SEG; ++j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          sigmoid_pair(W::get(zf[j], k), f[j][k], nf[j][k]);
+          g[j][k] = tanh_(W::get(zg[j], k));
+          o[j][k] = sigmoid_(W::get(zo[j], k));
+          before[j][k] = c[k];
+          c[k] = fmaf(f[j][k], c[k], nf[j][k] * g[j][k]);
+        }
+#pragma unroll
+      for (int j = SEG - 1; j >= 0; --j)
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const float A1 = A[k] * f[j][k], C1 = f[j][k] * fmaf(W::get(wy[j], k), o[j][k], C[k]);
+          A[k] = j < count ? A1 : A[k];
+          C[k] = j < count ? C1 : C[k];
+        }
+    }
+    link<V, NW>(sh.chain, set, lane, wave, -1, A, C, e, mine);
+    if (count > 0) {
+      float sum[3][V] = {};
+#pragma unroll
+      for (int j = SEG - 1; j >= 0; --j) {
+        if (j < count) {
+          float df[V], dg[V], dout[V];
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float dy = W::get(wy[j], k), now = fmaf(f[j][k], before[j][k], nf[j][k] * g[j][k]), dc = fmaf(dy, o[j][k], mine[k]);
+            mine[k] = f[j][k] * dc;
+            df[k] = (before[j][k] - g[j][k]) * nf[j][k] * mine[k];
+            dg[k] = dc * nf[j][k] * fmaf(-g[j][k], g[j][k], 1.f);
+            dout[k] = dy * now * fmaf(-o[j][k], o[j][k], o[j][k]);
+            sum[0][k] += df[k]; sum[1][k] += dg[k]; sum[2][k] += dout[k];
+          }
+          if (live) {
+            T* to = (T*)a.dz + (sp.row0 + (long)(s0 + j) * sp.step) * a.lddz;
+            W::store(to, at, df);
+            W::store(to + a.n, at, dg);
+            W::store(to + 2L * a.n, at, dout);
+          }
+        }
+      }
+#pragma unroll
+      for (int gate = 0; gate < 3; ++gate)
+#pragma unroll
+        for (int k = 0; k < V; ++k) total[gate][k] += (double)sum[gate][k];
+    }
+  }
+  if (live) {
+    float zero[V] = {};
+    for (int t = sp.L + part * NW + wave; t < a.T; t += a.parts * NW)
+      for (int gate = 0; gate < 3; ++gate) W::store((T*)a.dz + ((long)t * a.B + b) * a.lddz + (long)gate * a.n, at, zero);
+    if (a.dc0 && part == 0 && wave == 0) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) a.dc0[(long)b * a.n + u + k] = e[k];
+    }
+  }
+  if (!a.dbpart) return;
+  __syncthreads();                                              // (the chain's memory is used again)
+#pragma unroll
+  for (int gate = 0; gate < 3; ++gate)
+#pragma unroll
+    for (int k = 0; k < V; ++k) sh.sum[wave][gate][k][lane] = total[gate][k];
+  __syncthreads();
+  if (!live || wave != 0) return;
+  for (int gate = 0; gate < 3; ++gate)
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      double d = 0.0;
+      for (int w = 0; w < NW; ++w) d += sh.sum[w][gate][k][lane];
+      a.dbpart[(((long)part * a.B + b) * 3 + gate) * a.n + u + k] = d;
+    }
+}
+
+// The backward compositions of all parts but the first.
+template <typename T, int V, int NW, int SEG>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_bwd_join_kernel(ScanArgs a) {
+  typedef Word<T, V> W;
+  __shared__ Chain<V, NW> chain;
+  const int b = blockIdx.y, part = blockIdx.z + 1, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = (blockIdx.x * 64 + lane) * V;
+  const bool live = u < a.n;
+  const unsigned at = live ? u : 0;
+  const Span sp(a, b, part);
+  float A[V], C[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) { A[k] = 1.f; C[k] = 0.f; }
+  const int eighth = a.per / NW, from = sp.begin + wave * eighth, to = min(sp.end, from + eighth);
+  for (int s0 = from + (eighth / SEG - 1) * SEG; s0 >= from; s0 -= SEG) {
+    const int count = min(SEG, to - s0);
+    if (count <= 0) continue;
+    unsigned zf[SEG], zo[SEG], wy[SEG];
+#pragma unroll
+    for (int j = 0; j < SEG; ++j) {
+      const long r = sp.row0 + (long)(s0 + min(j, count - 1)) * sp.step;
+      const T* row = row_of<T>(a.z, r, a.ldz);
+      zf[j] = W::load(row, at);
+      zo[j] = W::load(row + 2L * a.n, at);
+      wy[j] = W::load(row_of<T>(a.dy, r, a.lddy), at);
+    }
+#pragma unroll
+    for (int j = SEG - 1; j >= 0; --j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float f = sigmoid_(W::get(zf[j], k)), A1 = A[k] * f, C1 = f * fmaf(W::get(wy[j], k), sigmoid_(W::get(zo[j], k)), C[k]);
+        A[k] = j < count ? A1 : A[k];
+        C[k] = j < count ? C1 : C[k];
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) { chain.a[0][wave][k][lane] = A[k]; chain.c[0][wave][k][lane] = C[k]; }
+  __syncthreads();
+  if (wave != 0 || !live) return;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float2 j = make_float2(1.f, 0.f);
+    for (int w = NW - 1; w >= 0; --w) {
+      j.x *= chain.a[0][w][k][lane];
+      j.y = fmaf(chain.a[0][w][k][lane], j.y, chain.c[0][w][k][lane]);
+    }
+    a.join[((long)part * a.B + b) * a.n + u + k] = j;
+  }
+}
+
+// db = the sum of `rows` rows of partial sums
+__global__ void scan_db_kernel(const double* __restrict__ part, float* __restrict__ db, int rows, int n3) {
+  const int i = blockIdx.x * 64 + threadIdx.x;
   if (i >= n3) return;
-  float s = 0.f;
-  for (int b = 0; b < B; ++b) s += part[(long)b * n3 + i];
-  db[i] = s;
+  double s = 0.0;
+  for (int r = 0; r < rows; ++r) s += part[(long)r * n3 + i];
+  db[i] = (float)s;
 }
 
 // Whole words of two values?
@@ -190,7 +439,35 @@ int scan_dims(int T, int B, int n) {
   return LSTM_OK;
 }
 uint64_t reserve_need(int T, int B, int n) { return (uint64_t)((T + kSeg - 1L) / kSeg) * B * n * 4 + 256; }
-uint64_t workspace_need(int B, int n) { return (uint64_t)B * n * 3 * 4 + 256; }
+
+// How the work is cut.  A wavefront takes 16 frames a round, so short batches have work-groups of fewer wavefronts; where rows and units give
+// too few work-groups for the device, time is cut into parts, whose compositions a launch before works out (a second reading of
+// two thirds of what the forward pass reads, three quarters of the backward pass).
+struct Cut { int V, waves, parts, per; };
+constexpr int kWaves = 8;
+Cut cut_of(int T, int B, int n, int V) {
+  Cut c = {V, T <= kSeg ? 1 : kWaves, 1, std::max(T, 1)};
+  const long groups = (long)cdiv(n, 64 * V) * B;
+  constexpr long kGroups = 512;
+  const int round = kWaves * kSeg;
+  if (groups > 0 && groups * 2 <= kGroups && T >= 4 * round) {
+    c.per = cdiv(cdiv(T, (int)std::min(kGroups / groups, (long)T / (2 * round))), round) * round;
+    c.parts = cdiv(T, c.per);
+  }
+  return c;
+}
+struct Places { uint64_t join, first, dbpart, total; };
+Places places_of(int T, int B, int n) {                          // (either width of a word: its address decides which is used)
+  const auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
+  const uint64_t parts = std::max(cut_of(T, B, n, 1).parts, cut_of(T, B, n, 2).parts), state = (uint64_t)B * n * 4;
+  Places p;
+  p.join = 0;
+  p.first = parts > 1 ? up(parts * state * 2) : 0;
+  p.dbpart = p.first + (parts > 1 ? up(state) : 0);
+  p.total = p.dbpart + up(parts * state * 6) + 256;
+  return p;
+}
+uint64_t workspace_need(int T, int B, int n) { return places_of(T, B, n).total; }
 int scan_kind(int dtype, int direction, int T, int B, int n) {
   const int rc = scan_dims(T, B, n);
   if (rc) return rc;
@@ -199,6 +476,37 @@ int scan_kind(int dtype, int direction, int T, int B, int n) {
   return LSTM_OK;
 }
 template <typename P> P* aligned(P* p) { return (P*)(((uintptr_t)p + 255) / 256 * 256); }
+void place(ScanArgs& a, const Cut& c, void* workspace) {
+  const Places p = places_of(a.T, a.B, a.n);
+  char* ws = aligned((char*)workspace);
+  a.join = (float2*)(ws + p.join); a.first = (float*)(ws + p.first); a.dbpart = (double*)(ws + p.dbpart);
+  a.parts = c.parts; a.per = c.per;
+}
+int status() { return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP; }
+
+template <typename T, int V>
+int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
+  const dim3 grid(cdiv(a.n, 64 * V), a.B, c.parts), most(grid.x, grid.y, c.parts - 1);
+  if (c.parts > 1) {
+    const auto join = gated_scan_join_kernel<T, V, kWaves, kSeg>;
+    hipLaunchKernelGGL(join, most, dim3(64 * kWaves), 0, s, a);
+  }
+  const auto kernel = a.T <= 1 ? gated_scan_fwd_kernel<T, V, 1, 1> : c.waves == 1 ? gated_scan_fwd_kernel<T, V, 1, kSeg> : gated_scan_fwd_kernel<T, V, kWaves, kSeg>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * c.waves), 0, s, a);
+  return status();
+}
+template <typename T, int V>
+int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
+  const dim3 grid(cdiv(a.n, 64 * V), a.B, c.parts), most(grid.x, grid.y, c.parts - 1);
+  if (c.parts > 1) {
+    const auto join = gated_scan_bwd_join_kernel<T, V, kWaves, kSeg>;
+    hipLaunchKernelGGL(join, most, dim3(64 * kWaves), 0, s, a);
+  }
+  const auto kernel = c.waves == 1 ? gated_scan_bwd_kernel<T, V, 1> : gated_scan_bwd_kernel<T, V, kWaves>;
+  if (a.B > 0) hipLaunchKernelGGL(kernel, grid, dim3(64 * c.waves), 0, s, a);
+  if (db) hipLaunchKernelGGL(scan_db_kernel, dim3(cdiv(3L * a.n, 64)), dim3(64), 0, s, a.dbpart, db, c.parts * a.B, 3 * a.n);
+  return status();
+}
 
 }  // namespace
 }  // namespace lstm
@@ -212,7 +520,7 @@ int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t
   const int rc = scan_dims(T, B, n);
   if (rc) return rc;
   *reserve_bytes = reserve_need(T, B, n);
-  *workspace_bytes = workspace_need(B, n);
+  *workspace_bytes = workspace_need(T, B, n);
   return LSTM_OK;
 }
 
@@ -225,17 +533,15 @@ int lstm_gated_scan_fwd(int dtype, int direction, int T, int B, int n, const voi
   if (ldz < 3L * n || ldy < n) return LSTM_ERR_DIM;
   if ((((uintptr_t)z | (uintptr_t)y) & (dtype == LSTM_F32 ? 3 : 1)) || (((uintptr_t)c0 | (uintptr_t)seq_lens | (uintptr_t)cT | (uintptr_t)reserve) & 3))
     return LSTM_ERR_ALIGN;
-  if ((reserve && reserve_bytes < reserve_need(T, B, n)) || workspace_bytes < workspace_need(B, n)) return LSTM_ERR_SIZE;
+  if ((reserve && reserve_bytes < reserve_need(T, B, n)) || workspace_bytes < workspace_need(T, B, n)) return LSTM_ERR_SIZE;
   if (B == 0) return LSTM_OK;
   if ((rc = device_ok())) return rc;
   ScanArgs a = {};
   a.z = z; a.ldz = ldz; a.c0 = c0; a.lens = seq_lens; a.y = y; a.ldy = ldy; a.cT = cT; a.kept = reserve ? aligned((float*)reserve) : nullptr;
   a.T = T; a.B = B; a.n = n; a.direction = direction;
-  const int V = dtype == LSTM_BF16_F32STATE && words(n, {ldz, ldy}, {z, y}) ? 2 : 1;
-  const auto kernel = dtype == LSTM_F32 ? gated_scan_fwd_kernel<float, 1> : V == 2 ? gated_scan_fwd_kernel<bf16_t, 2> : gated_scan_fwd_kernel<bf16_t, 1>;
-  hipLaunchKernelGGL(kernel,
-                     dim3(cdiv(n, 64 * V), B), dim3(64), 0, (hipStream_t)stream, a);
-  return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP;
+  const Cut c = cut_of(T, B, n, dtype == LSTM_BF16_F32STATE && words(n, {ldz, ldy}, {z, y}) ? 2 : 1);
+  place(a, c, workspace);
+  return dtype == LSTM_F32 ? run_fwd<float, 1>(a, c, (hipStream_t)stream) : c.V == 2 ? run_fwd<bf16_t, 2>(a, c, (hipStream_t)stream) : run_fwd<bf16_t, 1>(a, c, (hipStream_t)stream);
 }
 
 int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const int32_t* seq_lens, const void* reserve,
@@ -248,21 +554,17 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
   if ((((uintptr_t)z | (uintptr_t)dy | (uintptr_t)dz) & (dtype == LSTM_F32 ? 3 : 1)) ||
       (((uintptr_t)seq_lens | (uintptr_t)reserve | (uintptr_t)dcT | (uintptr_t)dc0 | (uintptr_t)db) & 3))
     return LSTM_ERR_ALIGN;
-  if (reserve_bytes < reserve_need(T, B, n) || workspace_bytes < workspace_need(B, n)) return LSTM_ERR_SIZE;
+  if (reserve_bytes < reserve_need(T, B, n) || workspace_bytes < workspace_need(T, B, n)) return LSTM_ERR_SIZE;
   if (B == 0 && !db) return LSTM_OK;
   if ((rc = device_ok())) return rc;
   hipStream_t s = (hipStream_t)stream;
   ScanArgs a = {};
   a.z = z; a.ldz = ldz; a.lens = seq_lens; a.kept = (float*)aligned((const float*)reserve); a.dy = dy; a.lddy = lddy; a.dcT = dcT; a.dz = dz; a.lddz = lddz;
-  a.dc0 = dc0; a.dbpart = db ? aligned((float*)workspace) : nullptr;
-  a.T = T; a.B = B; a.n = n; a.direction = direction;
-  const int V = dtype == LSTM_BF16_F32STATE && words(n, {ldz, lddy, lddz}, {z, dy, dz}) ? 2 : 1;
-  const auto kernel = dtype == LSTM_F32 ? gated_scan_bwd_kernel<float, 1> : V == 2 ? gated_scan_bwd_kernel<bf16_t, 2> : gated_scan_bwd_kernel<bf16_t, 1>;
-  if (B > 0)
-    hipLaunchKernelGGL(kernel,
-                       dim3(cdiv(n, 64 * V), B), dim3(64), 0, s, a);
-  if (db) hipLaunchKernelGGL(scan_db_kernel, dim3(cdiv(3L * n, 256)), dim3(256), 0, s, a.dbpart, db, B, 3 * n);
-  return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP;
+  a.dc0 = dc0; a.T = T; a.B = B; a.n = n; a.direction = direction;
+  const Cut c = cut_of(T, B, n, dtype == LSTM_BF16_F32STATE && words(n, {ldz, lddy, lddz}, {z, dy, dz}) ? 2 : 1);
+  place(a, c, workspace);
+  if (!db) a.dbpart = nullptr;
+  return dtype == LSTM_F32 ? run_bwd<float, 1>(a, c, db, s) : c.V == 2 ? run_bwd<bf16_t, 2>(a, c, db, s) : run_bwd<bf16_t, 1>(a, c, db, s);
 }
 
 }  // extern "C"
