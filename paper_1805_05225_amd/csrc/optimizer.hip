@@ -17,9 +17,10 @@ constexpr int kNormTile = 16384;      // elements whose squares a work-group add
 constexpr float kTop8 = 448.f;        // the largest e4m3 value
 
 // ---- the norm ---------------------------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 constexpr int kNormItems = 160;
 struct NormArgs {
-  struct Item { const void* g; long n; unsigned first; int bf16; } item[kNormItems];
+  struct Item { const void* g; long n; unsigned first; uint16_t bf16, wide; } item[kNormItems];
   double* part;                       // one per work-group
   int count;
 };
@@ -40,9 +41,31 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(NormArgs a) {
   const NormArgs::Item it = a.item[i];
   const long begin = (long)(blockIdx.x - it.first) * kNormTile, end = min(it.n, begin + kNormTile);
   double s = 0.0;
-  for (long k = begin + threadIdx.x; k < end; k += 256) {
-    const double g = it.bf16 ? Store<bf16_t>::load(it.g, k) : Store<float>::load(it.g, k);
-    s += g * g;
+  const auto square = [&](float x) { const double g = x; s = __builtin_fma(g, g, s); };
+  if (it.wide && end - begin == kNormTile) {                              // 16 bytes a load, all of a lane's in flight
+    constexpr int kLoads = kNormTile / 256 / 8;
+    if (it.bf16) {
+      u32x4 x[kLoads];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) x[u] = *(const u32x4*)((const uint16_t*)it.g + begin + 8 * (u * 256 + (int)threadIdx.x));
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { square(__uint_as_float(x[u][e] << 16)); square(__uint_as_float(x[u][e] & 0xffff0000u)); }
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        f32x4 x[kLoads];
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) x[u] = *(const f32x4*)((const float*)it.g + begin + 4 * ((half * kLoads + u) * 256 + (int)threadIdx.x));
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) square(x[u][e]);
+      }
+    }
+  } else {
+    for (long k = begin + threadIdx.x; k < end; k += 256) square(it.bf16 ? Store<bf16_t>::load(it.g, k) : Store<float>::load(it.g, k));
   }
   s = add_all(s, red);
   if (threadIdx.x == 0) a.part[blockIdx.x] = s;
@@ -60,15 +83,17 @@ __global__ __launch_bounds__(256) void grad_norm_sum_kernel(const double* __rest
 }
 
 // ---- AdamW ------------------------------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) bf16_t bf16x4;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 constexpr int kItems = 44;
 struct AdamArgs {
   struct Item {
     void* p; float* w; const void* g; void* m; void* v; float* ms; float* vs;
-    long n; float decay; unsigned first; int p_bf16, g_bf16;
+    long n; float decay; unsigned first; int p_bf16, g_bf16, wide;
   } item[kItems];
   int count, step;
   double lr, beta1, beta2;
-  float b1, nb1, b2, nb2, eps, rate, root2;        // beta, 1 - beta; lr / (1 - beta1^t) and sqrt(1 - beta2^t) unless lr or the step is in device memory
+  float b1, nb1, b2, nb2, eps, rate, inv_root2;    // beta, 1 - beta; lr / (1 - beta1^t) and 1 / sqrt(1 - beta2^t) unless lr or the step is in device memory
   const float* lr_dev; const int* step_dev; const float* grad_scale;
 };
 static_assert(sizeof(AdamArgs) <= 4096 && sizeof(NormArgs) <= 4096, "arguments of a launch");
@@ -81,9 +106,9 @@ __host__ __device__ inline double power(double beta, int t) {
   return r;
 }
 
-__host__ __device__ inline void corrections(double lr, double beta1, double beta2, int t, float& rate, float& root2) {
+__host__ __device__ inline void corrections(double lr, double beta1, double beta2, int t, float& rate, float& inv_root2) {
   rate = (float)(lr / (1.0 - power(beta1, t)));
-  root2 = (float)sqrt(1.0 - power(beta2, t));
+  inv_root2 = (float)(1.0 / sqrt(1.0 - power(beta2, t)));
 }
 
 __device__ __forceinline__ float wave_most(float x) {
@@ -91,14 +116,158 @@ __device__ __forceinline__ float wave_most(float x) {
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
   return x;
 }
-__device__ __forceinline__ float unit8(float x, float scale) {            // x in units of the block's scale
-  const float q = x / scale;
-  return x == 0.f ? 0.f : q != q ? q : fminf(fmaxf(q, -kTop8), kTop8);    // (0 / 0 where a block is all zeros; a NaN stays one)
+// Four values in units of a block's scale as e4m3 codes.  The quotient is the correctly rounded one (a code that depends on the last bit of an
+// approximation is another code than the formula's, and the next step sees it): from the scale's reciprocal, worked out once for the block, and
+// one correction by the remainder; by a division where the reciprocal of a tiny scale is infinite, or the scale is 0.
+struct Unit { float scale, inv; };
+__device__ __forceinline__ Unit unit_of(float scale) {
+  Unit u = {scale, __builtin_amdgcn_rcpf(scale)};
+  u.inv = fmaf(fmaf(-scale, u.inv, 1.f), u.inv, u.inv);
+  return u;
+}
+__device__ __forceinline__ unsigned pack8(const float (&x)[4], const Unit& u) {
+  float q[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    q[k] = x[k] * u.inv;
+    q[k] = fmaf(fmaf(-q[k], u.scale, x[k]), u.inv, q[k]);
+  }
+  if (!(u.scale > 1e-36f && u.scale < 1e36f)) {                            // (the same for the whole wavefront)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q[k] = x[k] == 0.f ? 0.f : x[k] / u.scale;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) q[k] = q[k] != q[k] ? q[k] : __builtin_amdgcn_fmed3f(q[k], -kTop8, kTop8);          // (a NaN stays one)
+  return __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), true);
+}
+
+// Four consecutive elements of an array of float or bfloat16.
+__device__ __forceinline__ void load4(const void* p, bool bf16, long at, float (&x)[4]) {
+  if (bf16) {
+    const u32x2 w = *(const u32x2*)((const uint16_t*)p + at);
+    x[0] = __uint_as_float(w[0] << 16); x[1] = __uint_as_float(w[0] & 0xffff0000u);
+    x[2] = __uint_as_float(w[1] << 16); x[3] = __uint_as_float(w[1] & 0xffff0000u);
+  } else {
+    const f32x4 w = *(const f32x4*)((const float*)p + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = w[k];
+  }
+}
+__device__ __forceinline__ void store4(void* p, bool bf16, long at, const float (&x)[4]) {
+  const f32x4 w = {x[0], x[1], x[2], x[3]};
+  if (bf16) *(bf16x4*)((bf16_t*)p + at) = __builtin_convertvector(w, bf16x4);
+  else *(f32x4*)((float*)p + at) = w;
+}
+
+// A work-group takes kTile elements of one tensor, a wavefront 256 of them at a time (a block of the 8-bit states), four consecutive ones a
+// lane.  WIDE: every array of the tensor starts at a multiple of four elements' bytes, and these 256 are all there; otherwise element by element.
+template <bool EIGHT, bool WIDE>
+__device__ __forceinline__ void adamw_block(const AdamArgs::Item& it, const AdamArgs& a, long block, int lane, float gs, float keep, float rate,
+                                            float inv_root2) {
+#pragma clang fp contract(off)                                            // every product and sum rounded by itself, as the formula is written
+  const long at = block * kBlock + 4 * lane;
+  float w[4], g[4], m[4], v[4], root[4];
+  int left = 4;
+  if (WIDE) {
+    load4(it.g, it.g_bf16, at, g);
+    if (it.w) load4(it.w, false, at, w); else load4(it.p, it.p_bf16, at, w);
+  } else {
+    left = (int)min(4L, max(0L, it.n - at));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const bool there = k < left;
+      g[k] = !there ? 0.f : it.g_bf16 ? Store<bf16_t>::load(it.g, at + k) : Store<float>::load(it.g, at + k);
+      w[k] = !there ? 0.f : it.w ? it.w[at + k] : it.p_bf16 ? Store<bf16_t>::load(it.p, at + k) : Store<float>::load(it.p, at + k);
+    }
+  }
+  if (EIGHT) {
+    unsigned cm = 0, cv = 0;
+    if (WIDE) {
+      cm = *(const unsigned*)((const uint8_t*)it.m + at);
+      cv = *(const unsigned*)((const uint8_t*)it.v + at);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) {
+          cm |= (unsigned)((const uint8_t*)it.m)[at + k] << (8 * k);
+          cv |= (unsigned)((const uint8_t*)it.v)[at + k] << (8 * k);
+        }
+    }
+    const float ms = it.ms[block], vs = it.vs[block];
+    m[0] = __builtin_amdgcn_cvt_f32_fp8(cm, 0); m[1] = __builtin_amdgcn_cvt_f32_fp8(cm, 1); m[2] = __builtin_amdgcn_cvt_f32_fp8(cm, 2); m[3] = __builtin_amdgcn_cvt_f32_fp8(cm, 3);
+    v[0] = __builtin_amdgcn_cvt_f32_fp8(cv, 0); v[1] = __builtin_amdgcn_cvt_f32_fp8(cv, 1); v[2] = __builtin_amdgcn_cvt_f32_fp8(cv, 2); v[3] = __builtin_amdgcn_cvt_f32_fp8(cv, 3);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] *= ms;
+      v[k] *= vs;
+      v[k] *= v[k];
+    }
+  } else if (WIDE) {
+    load4(it.m, false, at, m);
+    load4(it.v, false, at, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      m[k] = k < left ? ((const float*)it.m)[at + k] : 0.f;
+      v[k] = k < left ? ((const float*)it.v)[at + k] : 0.f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    g[k] *= gs;
+    m[k] = m[k] * a.b1 + g[k] * a.nb1;
+    v[k] = v[k] * a.b2 + (g[k] * a.nb2) * g[k];
+    // the quotient by the hardware's reciprocal (1 unit in the last place); the root too where it is not stored
+    root[k] = EIGHT ? sqrtf(v[k]) : __builtin_amdgcn_sqrtf(v[k]);
+    w[k] = w[k] * keep - (m[k] * __builtin_amdgcn_rcpf(root[k] * inv_root2 + a.eps)) * rate;
+  }
+  if (WIDE) {
+    if (it.w) store4(it.w, false, at, w);
+    store4(it.p, it.p_bf16, at, w);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < left) {
+        if (it.w) it.w[at + k] = w[k];
+        if (it.p_bf16) Store<bf16_t>::store(it.p, at + k, w[k]); else Store<float>::store(it.p, at + k, w[k]);
+      }
+  }
+  if (EIGHT) {
+    const float new_ms = wave_most(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))) * (1.f / kTop8);
+    const float new_vs = wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))) * (1.f / kTop8);
+    const unsigned cm = pack8(m, unit_of(new_ms));
+    unsigned cv = pack8(root, unit_of(new_vs));
+    // a positive root never becomes 0: code 1, 2^-9, is the smallest
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((cv >> (8 * k) & 255u) == 0u && root[k] > 0.f) cv |= 1u << (8 * k);
+    if (WIDE) {
+      *(unsigned*)((uint8_t*)it.m + at) = cm;
+      *(unsigned*)((uint8_t*)it.v + at) = cv;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < left) {
+          ((uint8_t*)it.m)[at + k] = (uint8_t)(cm >> (8 * k));
+          ((uint8_t*)it.v)[at + k] = (uint8_t)(cv >> (8 * k));
+        }
+    }
+    if (lane == 0) { it.ms[block] = new_ms; it.vs[block] = new_vs; }
+  } else if (WIDE) {
+    store4(it.m, false, at, m);
+    store4(it.v, false, at, v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < left) {
+        ((float*)it.m)[at + k] = m[k];
+        ((float*)it.v)[at + k] = v[k];
+      }
+  }
 }
 
 template <bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
-#pragma clang fp contract(off)                                            // every product and sum rounded by itself, as the formula is written
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   if (gs - gs != 0.f) return;                                             // NaN or infinite: the step is passed over
   int i = 0;
@@ -108,57 +277,19 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   }
   const AdamArgs::Item& it = a.item[i];
   const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
-  float rate = a.rate, root2 = a.root2;
-  if (a.lr_dev || a.step_dev) corrections(lr, a.beta1, a.beta2, a.step_dev ? max(*a.step_dev, 1) : a.step, rate, root2);
+  float rate = a.rate, inv_root2 = a.inv_root2;
+  if (a.lr_dev || a.step_dev) corrections(lr, a.beta1, a.beta2, a.step_dev ? max(*a.step_dev, 1) : a.step, rate, inv_root2);
   const float keep = (float)(1.0 - lr * it.decay);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int r = 0; r < kTile / kBlock / 4; ++r) {
-    const long block = (long)(blockIdx.x - it.first) * (kTile / kBlock) + r * 4 + wave, at = block * kBlock + 4 * lane;
-    if (block * kBlock >= it.n) return;
-    const float ms = EIGHT ? it.ms[block] : 1.f, vs = EIGHT ? it.vs[block] : 1.f;
-    float w[4], m[4], v[4], root[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long first = (long)(blockIdx.x - it.first) * (kTile / kBlock) + wave * (kTile / kBlock / 4);
+  if (it.wide && (first + kTile / kBlock / 4) * kBlock <= it.n) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      w[k] = m[k] = v[k] = root[k] = 0.f;
-      if (at + k >= it.n) continue;
-      w[k] = it.w ? it.w[at + k] : it.p_bf16 ? Store<bf16_t>::load(it.p, at + k) : Store<float>::load(it.p, at + k);
-      const float g = (it.g_bf16 ? Store<bf16_t>::load(it.g, at + k) : Store<float>::load(it.g, at + k)) * gs;
-      if (EIGHT) {
-        m[k] = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)it.m)[at + k], 0) * ms;
-        const float old = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)it.v)[at + k], 0) * vs;
-        v[k] = old * old;
-      } else {
-        m[k] = ((const float*)it.m)[at + k];
-        v[k] = ((const float*)it.v)[at + k];
-      }
-      m[k] = m[k] * a.b1 + g * a.nb1;
-      v[k] = v[k] * a.b2 + (g * a.nb2) * g;
-      root[k] = sqrtf(v[k]);
-      w[k] = w[k] * keep - (m[k] / (root[k] / root2 + a.eps)) * rate;
-      if (it.w) it.w[at + k] = w[k];
-      if (it.p_bf16) Store<bf16_t>::store(it.p, at + k, w[k]);
-      else Store<float>::store(it.p, at + k, w[k]);
-      if (!EIGHT) {
-        ((float*)it.m)[at + k] = m[k];
-        ((float*)it.v)[at + k] = v[k];
-      }
-    }
-    if (EIGHT) {
-      float top_m = 0.f, top_r = 0.f;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) { top_m = fmaxf(top_m, fabsf(m[k])); top_r = fmaxf(top_r, root[k]); }
-      const float new_ms = wave_most(top_m) * (1.f / kTop8), new_vs = wave_most(top_r) * (1.f / kTop8);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (at + k >= it.n) continue;
-        const int cm = __builtin_amdgcn_cvt_pk_fp8_f32(unit8(m[k], new_ms), 0.f, 0, false);
-        int cv = __builtin_amdgcn_cvt_pk_fp8_f32(unit8(root[k], new_vs), 0.f, 0, false) & 255;
-        if (cv == 0 && root[k] > 0.f) cv = 1;                             // the smallest code: 2^-9
-        ((uint8_t*)it.m)[at + k] = (uint8_t)cm;
-        ((uint8_t*)it.v)[at + k] = (uint8_t)cv;
-      }
-      if (lane == 0) { it.ms[block] = new_ms; it.vs[block] = new_vs; }
-    }
+    for (int r = 0; r < kTile / kBlock / 4; ++r) adamw_block<EIGHT, true>(it, a, first + r, lane, gs, keep, rate, inv_root2);
+    return;
+  }
+  for (int r = 0; r < kTile / kBlock / 4 && (first + r) * kBlock < it.n; ++r) {
+    if (it.wide && (first + r + 1) * kBlock <= it.n) adamw_block<EIGHT, true>(it, a, first + r, lane, gs, keep, rate, inv_root2);
+    else adamw_block<EIGHT, false>(it, a, first + r, lane, gs, keep, rate, inv_root2);
   }
 }
 
@@ -223,7 +354,7 @@ int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, floa
       if (a.count == kNormItems || first >= (1u << 24)) flush();
       const bool bf16 = items[i].grad_dtype == LSTM_BF16_F32STATE;
       const long n = std::min((long)items[i].count - at, kMost);
-      a.item[a.count++] = {(const char*)items[i].grad + at * (bf16 ? 2 : 4), n, first, bf16};
+      a.item[a.count++] = {(const char*)items[i].grad + at * (bf16 ? 2 : 4), n, first, bf16, ((uintptr_t)items[i].grad & 15) == 0};
       first += (unsigned)((n + kNormTile - 1) / kNormTile);
     }
   flush();
@@ -258,8 +389,8 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
   a.step = d->step; a.lr = d->lr; a.beta1 = d->beta1; a.beta2 = d->beta2;
   a.b1 = (float)d->beta1; a.nb1 = (float)(1.0 - d->beta1); a.b2 = (float)d->beta2; a.nb2 = (float)(1.0 - d->beta2); a.eps = (float)d->eps;
   a.lr_dev = d->lr_dev; a.step_dev = d->step_dev; a.grad_scale = d->grad_scale;
-  a.rate = a.root2 = 1.f;
-  if (!a.lr_dev && !a.step_dev) corrections(a.lr, a.beta1, a.beta2, a.step, a.rate, a.root2);
+  a.rate = a.inv_root2 = 1.f;
+  if (!a.lr_dev && !a.step_dev) corrections(a.lr, a.beta1, a.beta2, a.step, a.rate, a.inv_root2);
   unsigned first = 0;
   const auto flush = [&] {
     if (a.count > 0) hipLaunchKernelGGL(eight ? adamw_kernel<true> : adamw_kernel<false>, dim3(first), dim3(256), 0, (hipStream_t)stream, a);
@@ -272,9 +403,11 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
       const lstm_adamw_item& it = items[i];
       const bool pb = it.param_dtype == LSTM_BF16_F32STATE, gb = it.grad_dtype == LSTM_BF16_F32STATE;
       const long n = std::min((long)it.count - at, kMost), ss = at * (eight ? 1 : 4);
+      const bool wide = (((uintptr_t)it.param & (pb ? 7 : 15)) | ((uintptr_t)it.grad & (gb ? 7 : 15)) | ((uintptr_t)it.master & 15) |
+                         (((uintptr_t)it.m | (uintptr_t)it.v) & (eight ? 3 : 15))) == 0;
       a.item[a.count++] = {(char*)it.param + at * (pb ? 2 : 4), it.master ? it.master + at : nullptr, (const char*)it.grad + at * (gb ? 2 : 4),
                            (char*)it.m + ss, (char*)it.v + ss, eight ? it.m_scale + at / kBlock : nullptr, eight ? it.v_scale + at / kBlock : nullptr,
-                           n, it.weight_decay, first, pb, gb};
+                           n, it.weight_decay, first, pb, gb, wide};
       first += (unsigned)((n + kTile - 1) / kTile);
     }
   flush();
