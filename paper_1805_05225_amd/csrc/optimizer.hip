@@ -20,76 +20,102 @@ constexpr float kTop8 = 448.f;        // the largest e4m3 value
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 constexpr int kNormItems = 160;
 struct NormArgs {
-  struct Item { const void* g; long n; unsigned first; uint16_t bf16, wide; } item[kNormItems];
+  struct Item { const void* g; long n; unsigned first; int bf16; } item[kNormItems];
   double* part;                       // one per work-group
   int count;
 };
-__device__ __forceinline__ double add_all(double v, double* red) {      // the sum over a work-group of four wavefronts, in thread 0
+// the item that tile t belongs to
+template <typename Item> __device__ __forceinline__ int find(const Item* item, int count, unsigned t) {
+  int i = 0;
+  for (int hi = count; hi - i > 1;) {
+    const int mid = (i + hi) / 2;
+    if (t >= item[mid].first) i = mid; else hi = mid;
+  }
+  return i;
+}
+template <int NW = 4>
+__device__ __forceinline__ double add_all(double v, double* red) {      // the sum over a work-group of NW wavefronts, in thread 0
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return threadIdx.x == 0 ? (red[0] + red[1]) + (red[2] + red[3]) : 0.0;
+  double s = 0.0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < NW; ++w) s += red[w];
+  return s;
+}
+__device__ __forceinline__ void write_norm(double sum, float max_norm, float* out) {
+  const double norm = sqrt(sum);
+  out[0] = (float)norm;
+  out[1] = norm - norm != 0.0 ? __builtin_nanf("") : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+}
+// A thread's share of the sum of squares of elements [begin, end): whole pieces of 16 bytes between the first and the last such boundary, what lies
+// on either side one by one.  Eight loads of a thread are in flight together.
+template <int NT>
+__device__ __forceinline__ double squares(const void* g, long begin, long end, bool bf16, int tid) {
+  double s = 0.0;
+  const auto square = [&](float x) { const double d = x; s = __builtin_fma(d, d, s); };
+  const int size = bf16 ? 2 : 4;
+  const char* p = (const char*)g + begin * size;
+  const int n = (int)(end - begin), head = min(n, (int)(-(uintptr_t)p & 15) / size), per = 16 / size, pieces = (n - head) / per, tail = n - head - pieces * per;
+  if (tid < head + tail) {
+    const int at = tid < head ? tid : head + pieces * per + tid - head;
+    square(bf16 ? Store<bf16_t>::load(p, at) : Store<float>::load(p, at));
+  }
+  const u32x4* q = (const u32x4*)(p + head * size);
+  constexpr int U = 8;
+  for (int at = tid; at < pieces; at += U * NT) {
+    u32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = at + u * NT < pieces ? q[at + u * NT] : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        square(__uint_as_float(bf16 ? x[u][e] << 16 : x[u][e]));
+        if (bf16) square(__uint_as_float(x[u][e] & 0xffff0000u));
+      }
+  }
+  return s;
 }
 __global__ __launch_bounds__(256) void grad_norm_kernel(NormArgs a) {
   __shared__ double red[4];
-  int i = 0;
-  for (int hi = a.count; hi - i > 1;) {
-    const int mid = (i + hi) / 2;
-    if (blockIdx.x >= a.item[mid].first) i = mid; else hi = mid;
-  }
+  const int i = find(a.item, a.count, blockIdx.x);
   const NormArgs::Item it = a.item[i];
   const long begin = (long)(blockIdx.x - it.first) * kNormTile, end = min(it.n, begin + kNormTile);
-  double s = 0.0;
-  const auto square = [&](float x) { const double g = x; s = __builtin_fma(g, g, s); };
-  if (it.wide && end - begin == kNormTile) {                              // 16 bytes a load, all of a lane's in flight
-    constexpr int kLoads = kNormTile / 256 / 8;
-    if (it.bf16) {
-      u32x4 x[kLoads];
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) x[u] = *(const u32x4*)((const uint16_t*)it.g + begin + 8 * (u * 256 + (int)threadIdx.x));
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { square(__uint_as_float(x[u][e] << 16)); square(__uint_as_float(x[u][e] & 0xffff0000u)); }
-    } else {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        f32x4 x[kLoads];
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u) x[u] = *(const f32x4*)((const float*)it.g + begin + 4 * ((half * kLoads + u) * 256 + (int)threadIdx.x));
-#pragma unroll
-        for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) square(x[u][e]);
-      }
-    }
-  } else {
-    for (long k = begin + threadIdx.x; k < end; k += 256) square(it.bf16 ? Store<bf16_t>::load(it.g, k) : Store<float>::load(it.g, k));
-  }
-  s = add_all(s, red);
+  const double s = add_all(squares<256>(it.g, begin, end, it.bf16, threadIdx.x), red);
   if (threadIdx.x == 0) a.part[blockIdx.x] = s;
 }
-__global__ __launch_bounds__(256) void grad_norm_sum_kernel(const double* __restrict__ part, long count, float max_norm, float* __restrict__ out) {
-  __shared__ double red[4];
+__global__ __launch_bounds__(1024) void grad_norm_sum_kernel(const double* __restrict__ part, long count, float max_norm, float* __restrict__ out) {
+  __shared__ double red[16];
   double s = 0.0;
-  for (long k = threadIdx.x; k < count; k += 256) s += part[k];
-  s = add_all(s, red);
-  if (threadIdx.x == 0) {
-    const double norm = sqrt(s);
-    out[0] = (float)norm;
-    out[1] = norm - norm != 0.0 ? __builtin_nanf("") : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+  for (long k = threadIdx.x; k < count; k += 1024) s += part[k];
+  s = add_all<16>(s, red);
+  if (threadIdx.x == 0) write_norm(s, max_norm, out);
+}
+// Few elements: one work-group, one launch, its wavefronts taking kNormFewTile elements each.
+constexpr long kNormFew = 65536;
+constexpr int kNormFewTile = 2048;
+__global__ __launch_bounds__(1024) void grad_norm_few_kernel(NormArgs a, unsigned tiles, float max_norm, float* __restrict__ out) {
+  __shared__ double red[16];
+  double s = 0.0;
+  for (unsigned t = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); t < tiles; t += 16) {
+    const int i = find(a.item, a.count, t);
+    const long begin = (long)(t - a.item[i].first) * kNormFewTile;
+    s += squares<64>(a.item[i].g, begin, min(a.item[i].n, begin + kNormFewTile), a.item[i].bf16, threadIdx.x & 63);
   }
+  s = add_all<16>(s, red);
+  if (threadIdx.x == 0) write_norm(s, max_norm, out);
 }
 
 // ---- AdamW ------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) bf16_t bf16x4;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
-constexpr int kItems = 44;
+constexpr int kItems = 54;
 struct AdamArgs {
   struct Item {
     void* p; float* w; const void* g; void* m; void* v; float* ms; float* vs;
-    long n; float decay; unsigned first; int p_bf16, g_bf16, wide;
+    unsigned long n : 48, p_bf16 : 1, g_bf16 : 1, wide : 1; float decay; unsigned first;
   } item[kItems];
   int count, step;
   double lr, beta1, beta2;
@@ -159,83 +185,89 @@ __device__ __forceinline__ void store4(void* p, bool bf16, long at, const float 
   else *(f32x4*)((float*)p + at) = w;
 }
 
-// A work-group takes kTile elements of one tensor, a wavefront 256 of them at a time (a block of the 8-bit states), four consecutive ones a
-// lane.  WIDE: every array of the tensor starts at a multiple of four elements' bytes, and these 256 are all there; otherwise element by element.
+// What a lane holds of a block of 256 elements: four consecutive ones.
+template <bool EIGHT> struct Block {
+  float w[4], g[4];
+  float m[4], v[4];                   // (unused in 8 bits until they are worked out)
+  unsigned cm, cv;
+  float ms, vs;
+};
+// WIDE: every array of the tensor starts at a multiple of four elements' bytes, and the 256 elements are all there; otherwise element by element.
 template <bool EIGHT, bool WIDE>
-__device__ __forceinline__ void adamw_block(const AdamArgs::Item& it, const AdamArgs& a, long block, int lane, float gs, float keep, float rate,
-                                            float inv_root2) {
-#pragma clang fp contract(off)                                            // every product and sum rounded by itself, as the formula is written
+__device__ __forceinline__ void fetch(Block<EIGHT>& x, const AdamArgs::Item& it, long block, int lane) {
   const long at = block * kBlock + 4 * lane;
-  float w[4], g[4], m[4], v[4], root[4];
-  int left = 4;
   if (WIDE) {
-    load4(it.g, it.g_bf16, at, g);
-    if (it.w) load4(it.w, false, at, w); else load4(it.p, it.p_bf16, at, w);
+    load4(it.g, it.g_bf16, at, x.g);
+    if (it.w) load4(it.w, false, at, x.w); else load4(it.p, it.p_bf16, at, x.w);
+    if (EIGHT) {
+      x.cm = *(const unsigned*)((const uint8_t*)it.m + at);
+      x.cv = *(const unsigned*)((const uint8_t*)it.v + at);
+    } else {
+      load4(it.m, false, at, x.m);
+      load4(it.v, false, at, x.v);
+    }
   } else {
-    left = (int)min(4L, max(0L, it.n - at));
+    const int left = (int)min(4L, max(0L, (long)it.n - at));
+    x.cm = x.cv = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const bool there = k < left;
-      g[k] = !there ? 0.f : it.g_bf16 ? Store<bf16_t>::load(it.g, at + k) : Store<float>::load(it.g, at + k);
-      w[k] = !there ? 0.f : it.w ? it.w[at + k] : it.p_bf16 ? Store<bf16_t>::load(it.p, at + k) : Store<float>::load(it.p, at + k);
+      x.g[k] = !there ? 0.f : it.g_bf16 ? Store<bf16_t>::load(it.g, at + k) : Store<float>::load(it.g, at + k);
+      x.w[k] = !there ? 0.f : it.w ? it.w[at + k] : it.p_bf16 ? Store<bf16_t>::load(it.p, at + k) : Store<float>::load(it.p, at + k);
+      if (EIGHT) {
+        if (there) {
+          x.cm |= (unsigned)((const uint8_t*)it.m)[at + k] << (8 * k);
+          x.cv |= (unsigned)((const uint8_t*)it.v)[at + k] << (8 * k);
+        }
+      } else {
+        x.m[k] = there ? ((const float*)it.m)[at + k] : 0.f;
+        x.v[k] = there ? ((const float*)it.v)[at + k] : 0.f;
+      }
     }
   }
+  if (EIGHT) { x.ms = it.ms[block]; x.vs = it.vs[block]; }
+}
+template <bool EIGHT, bool WIDE>
+__device__ __forceinline__ void update(Block<EIGHT>& x, const AdamArgs::Item& it, const AdamArgs& a, long block, int lane, float gs, float keep, float rate,
+                                       float inv_root2) {
+#pragma clang fp contract(off)                                            // every product and sum rounded by itself, as the formula is written
+  const long at = block * kBlock + 4 * lane;
+  const int left = WIDE ? 4 : (int)min(4L, max(0L, (long)it.n - at));
+  float root[4];
   if (EIGHT) {
-    unsigned cm = 0, cv = 0;
-    if (WIDE) {
-      cm = *(const unsigned*)((const uint8_t*)it.m + at);
-      cv = *(const unsigned*)((const uint8_t*)it.v + at);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < left) {
-          cm |= (unsigned)((const uint8_t*)it.m)[at + k] << (8 * k);
-          cv |= (unsigned)((const uint8_t*)it.v)[at + k] << (8 * k);
-        }
-    }
-    const float ms = it.ms[block], vs = it.vs[block];
-    m[0] = __builtin_amdgcn_cvt_f32_fp8(cm, 0); m[1] = __builtin_amdgcn_cvt_f32_fp8(cm, 1); m[2] = __builtin_amdgcn_cvt_f32_fp8(cm, 2); m[3] = __builtin_amdgcn_cvt_f32_fp8(cm, 3);
-    v[0] = __builtin_amdgcn_cvt_f32_fp8(cv, 0); v[1] = __builtin_amdgcn_cvt_f32_fp8(cv, 1); v[2] = __builtin_amdgcn_cvt_f32_fp8(cv, 2); v[3] = __builtin_amdgcn_cvt_f32_fp8(cv, 3);
+    x.m[0] = __builtin_amdgcn_cvt_f32_fp8(x.cm, 0); x.m[1] = __builtin_amdgcn_cvt_f32_fp8(x.cm, 1); x.m[2] = __builtin_amdgcn_cvt_f32_fp8(x.cm, 2); x.m[3] = __builtin_amdgcn_cvt_f32_fp8(x.cm, 3);
+    x.v[0] = __builtin_amdgcn_cvt_f32_fp8(x.cv, 0); x.v[1] = __builtin_amdgcn_cvt_f32_fp8(x.cv, 1); x.v[2] = __builtin_amdgcn_cvt_f32_fp8(x.cv, 2); x.v[3] = __builtin_amdgcn_cvt_f32_fp8(x.cv, 3);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      m[k] *= ms;
-      v[k] *= vs;
-      v[k] *= v[k];
-    }
-  } else if (WIDE) {
-    load4(it.m, false, at, m);
-    load4(it.v, false, at, v);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      m[k] = k < left ? ((const float*)it.m)[at + k] : 0.f;
-      v[k] = k < left ? ((const float*)it.v)[at + k] : 0.f;
+      x.m[k] *= x.ms;
+      x.v[k] *= x.vs;
+      x.v[k] *= x.v[k];
     }
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    g[k] *= gs;
-    m[k] = m[k] * a.b1 + g[k] * a.nb1;
-    v[k] = v[k] * a.b2 + (g[k] * a.nb2) * g[k];
+    const float g = x.g[k] * gs;
+    x.m[k] = x.m[k] * a.b1 + g * a.nb1;
+    x.v[k] = x.v[k] * a.b2 + (g * a.nb2) * g;
     // the quotient by the hardware's reciprocal (1 unit in the last place); the root too where it is not stored
-    root[k] = EIGHT ? sqrtf(v[k]) : __builtin_amdgcn_sqrtf(v[k]);
-    w[k] = w[k] * keep - (m[k] * __builtin_amdgcn_rcpf(root[k] * inv_root2 + a.eps)) * rate;
+    root[k] = EIGHT ? sqrtf(x.v[k]) : __builtin_amdgcn_sqrtf(x.v[k]);
+    x.w[k] = x.w[k] * keep - (x.m[k] * __builtin_amdgcn_rcpf(root[k] * inv_root2 + a.eps)) * rate;
   }
   if (WIDE) {
-    if (it.w) store4(it.w, false, at, w);
-    store4(it.p, it.p_bf16, at, w);
+    if (it.w) store4(it.w, false, at, x.w);
+    store4(it.p, it.p_bf16, at, x.w);
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k < left) {
-        if (it.w) it.w[at + k] = w[k];
-        if (it.p_bf16) Store<bf16_t>::store(it.p, at + k, w[k]); else Store<float>::store(it.p, at + k, w[k]);
+        if (it.w) it.w[at + k] = x.w[k];
+        if (it.p_bf16) Store<bf16_t>::store(it.p, at + k, x.w[k]); else Store<float>::store(it.p, at + k, x.w[k]);
       }
   }
   if (EIGHT) {
-    const float new_ms = wave_most(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))) * (1.f / kTop8);
+    const float new_ms = wave_most(fmaxf(fmaxf(fabsf(x.m[0]), fabsf(x.m[1])), fmaxf(fabsf(x.m[2]), fabsf(x.m[3])))) * (1.f / kTop8);
     const float new_vs = wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))) * (1.f / kTop8);
-    const unsigned cm = pack8(m, unit_of(new_ms));
+    const unsigned cm = pack8(x.m, unit_of(new_ms));
     unsigned cv = pack8(root, unit_of(new_vs));
     // a positive root never becomes 0: code 1, 2^-9, is the smallest
 #pragma unroll
@@ -254,27 +286,25 @@ __device__ __forceinline__ void adamw_block(const AdamArgs::Item& it, const Adam
     }
     if (lane == 0) { it.ms[block] = new_ms; it.vs[block] = new_vs; }
   } else if (WIDE) {
-    store4(it.m, false, at, m);
-    store4(it.v, false, at, v);
+    store4(it.m, false, at, x.m);
+    store4(it.v, false, at, x.v);
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (k < left) {
-        ((float*)it.m)[at + k] = m[k];
-        ((float*)it.v)[at + k] = v[k];
+        ((float*)it.m)[at + k] = x.m[k];
+        ((float*)it.v)[at + k] = x.v[k];
       }
   }
 }
 
+// A work-group takes kTile elements of one tensor, a wavefront a quarter of them, 256 at a time (a block of the 8-bit states); what it reads of
+// all four is asked for before the first is worked on.
 template <bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   if (gs - gs != 0.f) return;                                             // NaN or infinite: the step is passed over
-  int i = 0;
-  for (int hi = a.count; hi - i > 1;) {
-    const int mid = (i + hi) / 2;
-    if (blockIdx.x >= a.item[mid].first) i = mid; else hi = mid;
-  }
+  const int i = find(a.item, a.count, blockIdx.x);
   const AdamArgs::Item& it = a.item[i];
   const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
   float rate = a.rate, inv_root2 = a.inv_root2;
@@ -282,14 +312,26 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const float keep = (float)(1.0 - lr * it.decay);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long first = (long)(blockIdx.x - it.first) * (kTile / kBlock) + wave * (kTile / kBlock / 4);
-  if (it.wide && (first + kTile / kBlock / 4) * kBlock <= it.n) {
+  constexpr int kMine = kTile / kBlock / 4;
+  const long n = it.n;
+  const bool wide = it.wide;
+  Block<EIGHT> x[kMine];
+  if (wide && (first + kMine) * kBlock <= n) {
 #pragma unroll
-    for (int r = 0; r < kTile / kBlock / 4; ++r) adamw_block<EIGHT, true>(it, a, first + r, lane, gs, keep, rate, inv_root2);
+    for (int r = 0; r < kMine; ++r) fetch<EIGHT, true>(x[r], it, first + r, lane);
+#pragma unroll
+    for (int r = 0; r < kMine; ++r) update<EIGHT, true>(x[r], it, a, first + r, lane, gs, keep, rate, inv_root2);
     return;
   }
-  for (int r = 0; r < kTile / kBlock / 4 && (first + r) * kBlock < it.n; ++r) {
-    if (it.wide && (first + r + 1) * kBlock <= it.n) adamw_block<EIGHT, true>(it, a, first + r, lane, gs, keep, rate, inv_root2);
-    else adamw_block<EIGHT, false>(it, a, first + r, lane, gs, keep, rate, inv_root2);
+#pragma unroll
+  for (int r = 0; r < kMine; ++r) {
+    if (wide && (first + r + 1) * kBlock <= n) fetch<EIGHT, true>(x[r], it, first + r, lane);
+    else if ((first + r) * kBlock < n) fetch<EIGHT, false>(x[r], it, first + r, lane);
+  }
+#pragma unroll
+  for (int r = 0; r < kMine; ++r) {
+    if (wide && (first + r + 1) * kBlock <= n) update<EIGHT, true>(x[r], it, a, first + r, lane, gs, keep, rate, inv_root2);
+    else if ((first + r) * kBlock < n) update<EIGHT, false>(x[r], it, a, first + r, lane, gs, keep, rate, inv_root2);
   }
 }
 
@@ -349,16 +391,23 @@ int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, floa
     a.part += first;
     a.count = 0; first = 0;
   };
+  long elements = 0;
+  for (int i = 0; i < count; ++i) elements += items[i].count;
+  const bool few = elements <= kNormFew && count <= kNormItems;
   for (int i = 0; i < count; ++i)
     for (long at = 0; at < items[i].count; at += kMost) {
       if (a.count == kNormItems || first >= (1u << 24)) flush();
       const bool bf16 = items[i].grad_dtype == LSTM_BF16_F32STATE;
       const long n = std::min((long)items[i].count - at, kMost);
-      a.item[a.count++] = {(const char*)items[i].grad + at * (bf16 ? 2 : 4), n, first, bf16, ((uintptr_t)items[i].grad & 15) == 0};
-      first += (unsigned)((n + kNormTile - 1) / kNormTile);
+      a.item[a.count++] = {(const char*)items[i].grad + at * (bf16 ? 2 : 4), n, first, bf16};
+      first += (unsigned)(few ? (n + kNormFewTile - 1) / kNormFewTile : (n + kNormTile - 1) / kNormTile);
     }
+  if (few) {
+    hipLaunchKernelGGL(grad_norm_few_kernel, dim3(1), dim3(1024), 0, s, a, first, max_norm, out);
+    return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP;
+  }
   flush();
-  hipLaunchKernelGGL(grad_norm_sum_kernel, dim3(1), dim3(256), 0, s, part, (long)groups, max_norm, out);
+  hipLaunchKernelGGL(grad_norm_sum_kernel, dim3(1), dim3(1024), 0, s, part, (long)groups, max_norm, out);
   return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP;
 }
 
@@ -407,7 +456,7 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
                          (((uintptr_t)it.m | (uintptr_t)it.v) & (eight ? 3 : 15))) == 0;
       a.item[a.count++] = {(char*)it.param + at * (pb ? 2 : 4), it.master ? it.master + at : nullptr, (const char*)it.grad + at * (gb ? 2 : 4),
                            (char*)it.m + ss, (char*)it.v + ss, eight ? it.m_scale + at / kBlock : nullptr, eight ? it.v_scale + at / kBlock : nullptr,
-                           n, it.weight_decay, first, pb, gb, wide};
+                           (unsigned long)n, pb, gb, wide, it.weight_decay, first};
       first += (unsigned)((n + kTile - 1) / kTile);
     }
   flush();
