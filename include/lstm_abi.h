@@ -311,11 +311,12 @@ int lstm_embed(int B, int n, int V, const int32_t* label, const void* W_trg, con
  *   -> dz [T][B][lddz >= 3n]; dc0 [B][n] or NULL (not wanted); db [3n], the sum of dz over all valid frames before its rounding, or NULL.
  * The gradients of x and W are products of dz (lstm_gemm, with seq_lens masking the frames).  Rows may start at any element; whole words of
  * two bfloat16 values (even n, ld and addresses of whole words) are faster.  T == 0 or B == 0 is legal: cT = c0, dc0 = dcT, db = 0.
- * Only cT may overlap an input (c0).  workspace: workspace_bytes of the query, for either call; nothing in it has to survive a call.
+ * Only cT may overlap an input (c0).  workspace: fwd_workspace_bytes or bwd_workspace_bytes of the query, nothing (NULL) where that is 0; nothing in
+ * it has to survive a call.
  * Calls with the same inputs agree bit for bit.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative T or B, n < 1, ld too small, more than 2^31 - 1 rows or states), LSTM_ERR_DIRECTION, LSTM_ERR_UNSUPPORTED
  * (dtype), LSTM_ERR_ALIGN (element alignment), LSTM_ERR_SIZE (reserve or workspace), LSTM_ERR_HIP. */
-int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* workspace_bytes);
+int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* fwd_workspace_bytes, uint64_t* bwd_workspace_bytes);
 int lstm_gated_scan_fwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const float* c0, const int32_t* seq_lens,
                         void* y, int64_t ldy, float* cT, void* reserve, uint64_t reserve_bytes, void* workspace, uint64_t workspace_bytes,
                         void* stream);
@@ -341,7 +342,8 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *   Forward: label and logp may both be NULL, entropy and stats may be; top_logp and top_label may be NULL with top = 0 only.
  *   Backward: stats (and entropy, with dent) from the forward call; dlogp, dent float [T][B] or NULL (zeros); label may be NULL without dlogp;
  *   dlogits [T][B][ldd >= V], which may be logits (with ldd = ld).
- *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call); nothing in it has to survive a call.
+ *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call; nothing, NULL, where
+ *   that is 0); nothing in it has to survive a call.
  * Calls with the same inputs agree bit for bit.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0), LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN,
  * LSTM_ERR_SIZE, LSTM_ERR_HIP. */

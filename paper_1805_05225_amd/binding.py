@@ -101,7 +101,7 @@ def _load():
     lib.lstm_embed.argtypes = [ip, ip, ip, vp, vp, vp, vp, i64, vp]
     u64 = ctypes.c_uint64
     lib.lstm_gated_scan_query.restype = ip
-    lib.lstm_gated_scan_query.argtypes = [ip, ip, ip, u64p, u64p]
+    lib.lstm_gated_scan_query.argtypes = [ip, ip, ip, u64p, u64p, u64p]
     lib.lstm_gated_scan_fwd.restype = ip
     lib.lstm_gated_scan_fwd.argtypes = [ip] * 5 + [vp, i64, vp, vp, vp, i64, vp, vp, u64, vp, u64, vp]
     lib.lstm_gated_scan_bwd.restype = ip
@@ -307,10 +307,10 @@ def embed(label, W_trg, b_trg=None, *, out=None):
 
 
 def gated_scan_query(T, B, n):
-    """-> bytes of reserve and of workspace."""
-    r, w = ctypes.c_uint64(0), ctypes.c_uint64(0)
-    _check(lib.lstm_gated_scan_query(T, B, n, ctypes.byref(r), ctypes.byref(w)))
-    return r.value, w.value
+    """-> bytes of reserve, of the forward call's workspace and of the backward call's."""
+    got = [ctypes.c_uint64(0) for _ in range(3)]
+    _check(lib.lstm_gated_scan_query(T, B, n, *[ctypes.byref(g) for g in got]))
+    return tuple(g.value for g in got)
 
 
 def gated_scan_fwd(z, c0=None, seq_lens=None, *, direction=1, save=True, want_state=True, out=None, workspace=None):

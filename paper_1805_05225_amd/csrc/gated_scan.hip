@@ -493,18 +493,20 @@ Cut cut_of(int T, int B, int n, int V) {
   }
   return c;
 }
+// What the parts of a call leave each other in the workspace.
 struct Places { uint64_t join, first, dbpart, total; };
-Places places_of(int T, int B, int n) {                          // (either width of a word: its address decides which is used)
+Places places_of(int T, int B, int n, bool backward) {           // (for either width of a word: the rows' addresses decide which is used)
   const auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
   const uint64_t parts = std::max(cut_of(T, B, n, 1).parts, cut_of(T, B, n, 2).parts), state = (uint64_t)B * n * 4;
   Places p;
   p.join = 0;
   p.first = parts > 1 ? up(parts * state * 2) : 0;
   p.dbpart = p.first + (parts > 1 ? up(state) : 0);
-  p.total = p.dbpart + up(parts * state * 6) + 256;
+  p.total = p.dbpart + (backward ? up(parts * state * 6) : 0);
+  if (p.total > 0) p.total += 256;
   return p;
 }
-uint64_t workspace_need(int T, int B, int n) { return places_of(T, B, n).total; }
+uint64_t workspace_need(int T, int B, int n, bool backward) { return places_of(T, B, n, backward).total; }
 int scan_kind(int dtype, int direction, int T, int B, int n) {
   const int rc = scan_dims(T, B, n);
   if (rc) return rc;
@@ -513,8 +515,8 @@ int scan_kind(int dtype, int direction, int T, int B, int n) {
   return LSTM_OK;
 }
 template <typename P> P* aligned(P* p) { return (P*)(((uintptr_t)p + 255) / 256 * 256); }
-void place(ScanArgs& a, const Cut& c, void* workspace) {
-  const Places p = places_of(a.T, a.B, a.n);
+void place(ScanArgs& a, const Cut& c, void* workspace, bool backward) {
+  const Places p = places_of(a.T, a.B, a.n, backward);
   char* ws = aligned((char*)workspace);
   a.join = (float2*)(ws + p.join); a.first = (float*)(ws + p.first); a.dbpart = (double*)(ws + p.dbpart);
   a.parts = c.parts; a.per = c.per;
@@ -552,46 +554,51 @@ using namespace lstm;
 
 extern "C" {
 
-int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* workspace_bytes) {
-  if (!reserve_bytes || !workspace_bytes) return LSTM_ERR_NULL;
+int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* fwd_workspace_bytes, uint64_t* bwd_workspace_bytes) {
+  if (!reserve_bytes || !fwd_workspace_bytes || !bwd_workspace_bytes) return LSTM_ERR_NULL;
   const int rc = scan_dims(T, B, n);
   if (rc) return rc;
   *reserve_bytes = reserve_need(T, B, n);
-  *workspace_bytes = workspace_need(T, B, n);
+  *fwd_workspace_bytes = workspace_need(T, B, n, false);
+  *bwd_workspace_bytes = workspace_need(T, B, n, true);
   return LSTM_OK;
 }
 
 int lstm_gated_scan_fwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const float* c0, const int32_t* seq_lens,
                         void* y, int64_t ldy, float* cT, void* reserve, uint64_t reserve_bytes, void* workspace, uint64_t workspace_bytes,
                         void* stream) {
-  if (((!z || !y) && T > 0 && B > 0) || !workspace) return LSTM_ERR_NULL;      // (arrays without elements may have no address)
+  if ((!z || !y) && T > 0 && B > 0) return LSTM_ERR_NULL;        // (arrays without elements may have no address)
   int rc = scan_kind(dtype, direction, T, B, n);
   if (rc) return rc;
   if (ldz < 3L * n || ldy < n) return LSTM_ERR_DIM;
   if ((((uintptr_t)z | (uintptr_t)y) & (dtype == LSTM_F32 ? 3 : 1)) || (((uintptr_t)c0 | (uintptr_t)seq_lens | (uintptr_t)cT | (uintptr_t)reserve) & 3))
     return LSTM_ERR_ALIGN;
-  if ((reserve && reserve_bytes < reserve_need(T, B, n)) || workspace_bytes < workspace_need(T, B, n)) return LSTM_ERR_SIZE;
+  const uint64_t need = workspace_need(T, B, n, false);
+  if (need > 0 && !workspace) return LSTM_ERR_NULL;
+  if ((reserve && reserve_bytes < reserve_need(T, B, n)) || workspace_bytes < need) return LSTM_ERR_SIZE;
   if (B == 0) return LSTM_OK;
   if ((rc = device_ok())) return rc;
   ScanArgs a = {};
   a.z = z; a.ldz = ldz; a.c0 = c0; a.lens = seq_lens; a.y = y; a.ldy = ldy; a.cT = cT; a.kept = reserve ? aligned((float*)reserve) : nullptr;
   a.T = T; a.B = B; a.n = n; a.direction = direction;
   const Cut c = cut_of(T, B, n, dtype == LSTM_BF16_F32STATE && words(n, {ldz, ldy}, {z, y}) ? 2 : 1);
-  place(a, c, workspace);
+  place(a, c, workspace, false);
   return dtype == LSTM_F32 ? run_fwd<float, 1>(a, c, (hipStream_t)stream) : c.V == 2 ? run_fwd<bf16_t, 2>(a, c, (hipStream_t)stream) : run_fwd<bf16_t, 1>(a, c, (hipStream_t)stream);
 }
 
 int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const int32_t* seq_lens, const void* reserve,
                         uint64_t reserve_bytes, const void* dy, int64_t lddy, const float* dcT, void* dz, int64_t lddz, float* dc0, float* db,
                         void* workspace, uint64_t workspace_bytes, void* stream) {
-  if (((!z || !dy || !dz) && T > 0 && B > 0) || !reserve || !workspace) return LSTM_ERR_NULL;
+  if (((!z || !dy || !dz) && T > 0 && B > 0) || !reserve) return LSTM_ERR_NULL;
   int rc = scan_kind(dtype, direction, T, B, n);
   if (rc) return rc;
   if (ldz < 3L * n || lddy < n || lddz < 3L * n) return LSTM_ERR_DIM;
   if ((((uintptr_t)z | (uintptr_t)dy | (uintptr_t)dz) & (dtype == LSTM_F32 ? 3 : 1)) ||
       (((uintptr_t)seq_lens | (uintptr_t)reserve | (uintptr_t)dcT | (uintptr_t)dc0 | (uintptr_t)db) & 3))
     return LSTM_ERR_ALIGN;
-  if (reserve_bytes < reserve_need(T, B, n) || workspace_bytes < workspace_need(T, B, n)) return LSTM_ERR_SIZE;
+  const uint64_t need = workspace_need(T, B, n, true);
+  if (need > 0 && !workspace) return LSTM_ERR_NULL;
+  if (reserve_bytes < reserve_need(T, B, n) || workspace_bytes < need) return LSTM_ERR_SIZE;
   if (B == 0 && !db) return LSTM_OK;
   if ((rc = device_ok())) return rc;
   hipStream_t s = (hipStream_t)stream;
@@ -599,7 +606,7 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
   a.z = z; a.ldz = ldz; a.lens = seq_lens; a.kept = (float*)aligned((const float*)reserve); a.dy = dy; a.lddy = lddy; a.dcT = dcT; a.dz = dz; a.lddz = lddz;
   a.dc0 = dc0; a.T = T; a.B = B; a.n = n; a.direction = direction;
   const Cut c = cut_of(T, B, n, dtype == LSTM_BF16_F32STATE && words(n, {ldz, lddy, lddz}, {z, dy, dz}) ? 2 : 1);
-  place(a, c, workspace);
+  place(a, c, workspace, true);
   if (!db) a.dbpart = nullptr;
   return dtype == LSTM_F32 ? run_bwd<float, 1>(a, c, db, s) : c.V == 2 ? run_bwd<bf16_t, 2>(a, c, db, s) : run_bwd<bf16_t, 1>(a, c, db, s);
 }

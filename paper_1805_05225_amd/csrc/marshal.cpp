@@ -381,13 +381,16 @@ int64_t row_stride(const at::Tensor& t, const char* what) {
   require(T == 1 || t.stride(0) == B * ld, what);
   return ld;
 }
-// workspace of `need` bytes: `o` if it is given (the library checks its size), otherwise a new one
+// workspace of `need` bytes: `o` if it is given (the library checks its size), otherwise a new one, or none if nothing is needed
 at::Tensor scratch_of(PyObject* o, const at::Tensor& like, uint64_t need, long device) {
-  if (o == Py_None) return bytes_like(like, (int64_t)need);
+  if (o == Py_None) return need == 0 ? at::Tensor() : bytes_like(like, (int64_t)need);
   const at::Tensor& t = placed(o, device, kWhere);
   require(t.is_contiguous() && t.scalar_type() == at::kByte, "a workspace is a contiguous tensor of bytes");
   return t;
 }
+
+void* address(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+uint64_t size_of(const at::Tensor& t) { return t.defined() ? (uint64_t)t.numel() : 0; }
 
 // z c0 lens | direction save want_state out workspace device stream  -> (status, y, cT, reserve, workspace)
 FAST(gated_scan_fwd) {
@@ -396,8 +399,8 @@ FAST(gated_scan_fwd) {
     const at::Tensor& z = placed(a[0], dev, kWhere);
     require(z.dim() == 3 && z.size(2) % 3 == 0 && stored(z), "z is [T, B, 3n], float or bfloat16");
     const int64_t T = z.size(0), B = z.size(1), n = z.size(2) / 3, ldz = row_stride(z, "rows of z are contiguous and evenly spaced");
-    uint64_t rb = 0, wb = 0;
-    int rc = T > INT32_MAX || B > INT32_MAX || n > INT32_MAX ? (int)LSTM_ERR_DIM : abi.scan_query((int)T, (int)B, (int)n, &rb, &wb);
+    uint64_t rb = 0, fb = 0, bb = 0;
+    int rc = T > INT32_MAX || B > INT32_MAX || n > INT32_MAX ? (int)LSTM_ERR_DIM : abi.scan_query((int)T, (int)B, (int)n, &rb, &fb, &bb);
     if (rc) return Py_BuildValue("(i)", rc);
     const float* c0 = whole<float>(a[1], dev, at::kFloat, B * n, "c0 is a contiguous float [B, n]");
     const int32_t* lens = whole<int32_t>(a[2], dev, at::kInt, B, "seq_lens is a contiguous int32 [B]");
@@ -407,9 +410,9 @@ FAST(gated_scan_fwd) {
     at::Tensor cT, reserve;
     if (truth(a[5])) cT = at::empty({B, n}, z.options().dtype(at::kFloat));
     if (truth(a[4])) reserve = bytes_like(z, (int64_t)rb);
-    const at::Tensor ws = scratch_of(a[7], z, wb, dev);
+    const at::Tensor ws = scratch_of(a[7], z, fb, dev);
     rc = call(abi.scan_fwd, storage(z), (int)integer(a[3]), (int)T, (int)B, (int)n, z.data_ptr(), ldz, c0, lens, y.data_ptr(), ldy,
-              cT.defined() ? (float*)cT.data_ptr() : nullptr, reserve.defined() ? reserve.data_ptr() : nullptr, rb, ws.data_ptr(), (uint64_t)ws.numel(),
+              cT.defined() ? (float*)cT.data_ptr() : nullptr, reserve.defined() ? reserve.data_ptr() : nullptr, rb, address(ws), size_of(ws),
               stream_of(a[9]));
     return Py_BuildValue("(iNNNN)", rc, wrapped(y), wrapped(cT), wrapped(reserve), wrapped(ws));
   });
@@ -422,8 +425,8 @@ FAST(gated_scan_bwd) {
     const at::Tensor &z = placed(a[0], dev, kWhere), &reserve = placed(a[2], dev, kWhere), &dy = placed(a[3], dev, kWhere);
     require(z.dim() == 3 && z.size(2) % 3 == 0 && stored(z), "z is [T, B, 3n], float or bfloat16");
     const int64_t T = z.size(0), B = z.size(1), n = z.size(2) / 3, ldz = row_stride(z, "rows of z are contiguous and evenly spaced");
-    uint64_t rb = 0, wb = 0;
-    int rc = T > INT32_MAX || B > INT32_MAX || n > INT32_MAX ? (int)LSTM_ERR_DIM : abi.scan_query((int)T, (int)B, (int)n, &rb, &wb);
+    uint64_t rb = 0, fb = 0, bb = 0;
+    int rc = T > INT32_MAX || B > INT32_MAX || n > INT32_MAX ? (int)LSTM_ERR_DIM : abi.scan_query((int)T, (int)B, (int)n, &rb, &fb, &bb);
     if (rc) return Py_BuildValue("(i)", rc);
     require(dy.dim() == 3 && dy.size(0) == T && dy.size(1) == B && dy.size(2) == n && dy.scalar_type() == z.scalar_type(), "dy is [T, B, n] of z's type");
     const int64_t lddy = row_stride(dy, "rows of dy are contiguous and evenly spaced");
@@ -437,10 +440,10 @@ FAST(gated_scan_bwd) {
     at::Tensor dc0, db;
     if (truth(a[6])) dc0 = at::empty({B, n}, f32);
     if (truth(a[7])) db = at::empty({3 * n}, f32);
-    const at::Tensor ws = scratch_of(a[9], z, wb, dev);
+    const at::Tensor ws = scratch_of(a[9], z, bb, dev);
     rc = call(abi.scan_bwd, storage(z), (int)integer(a[5]), (int)T, (int)B, (int)n, z.data_ptr(), ldz, lens, reserve.data_ptr(), (uint64_t)reserve.numel(),
               dy.data_ptr(), lddy, dcT, dz.data_ptr(), lddz, dc0.defined() ? (float*)dc0.data_ptr() : nullptr, db.defined() ? (float*)db.data_ptr() : nullptr,
-              ws.data_ptr(), (uint64_t)ws.numel(), stream_of(a[11]));
+              address(ws), size_of(ws), stream_of(a[11]));
     return Py_BuildValue("(iNNN)", rc, wrapped(dz), wrapped(dc0), wrapped(db));
   });
 }
@@ -480,7 +483,7 @@ FAST(label_score_fwd) {
     const at::Tensor ws = scratch_of(a[5], x, need, dev);
     const auto p = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
     rc = call(abi.score_fwd, storage(x), (int)s.T, (int)s.B, (int)s.V, x.data_ptr(), s.ld, label, lens, (float*)p(logp), (float*)p(entropy), (float*)p(stats),
-              (int)top, (float*)p(top_logp), (int32_t*)p(top_label), ws.data_ptr(), (uint64_t)ws.numel(), stream_of(a[7]));
+              (int)top, (float*)p(top_logp), (int32_t*)p(top_label), address(ws), size_of(ws), stream_of(a[7]));
     return Py_BuildValue("(iNNNNNN)", rc, wrapped(logp), wrapped(entropy), wrapped(stats), wrapped(top_logp), wrapped(top_label), wrapped(ws));
   });
 }
@@ -509,21 +512,28 @@ FAST(label_score_bwd) {
 // The tensors of an update, read from sequences (None: not given), held until the call has returned.
 struct Update {
   std::vector<lstm_adamw_item> item;
-  std::vector<at::Tensor> held;
+  std::vector<PyObject*> held;
   long device;
   explicit Update(long dev) : device(dev) {}
+  ~Update() {
+    for (PyObject* o : held) Py_DECREF(o);
+  }
+  PyObject* object(PyObject* seq, Py_ssize_t i) {
+    PyObject* o = PySequence_GetItem(seq, i);
+    if (!o) throw Failed();
+    held.push_back(o);
+    return o;
+  }
   const at::Tensor& at_index(PyObject* seq, Py_ssize_t i) {
-    struct Ref { PyObject* o; ~Ref() { Py_XDECREF(o); } } ref{PySequence_GetItem(seq, i)};
-    if (!ref.o) throw Failed();
-    held.push_back(placed(ref.o, device, kWhere));
-    require(held.back().is_contiguous(), "tensors crossing the ABI must be contiguous");
-    return held.back();
+    const at::Tensor& t = placed(object(seq, i), device, kWhere);
+    require(t.is_contiguous(), "tensors crossing the ABI must be contiguous");
+    return t;
   }
   void grads(PyObject* seq) {
     const Py_ssize_t count = PySequence_Size(seq);
     if (count < 0) throw Failed();
     item.resize(count);
-    held.reserve(7 * count);
+    held.reserve(8 * count);
     for (Py_ssize_t i = 0; i < count; ++i) {
       const at::Tensor& t = at_index(seq, i);
       require(stored(t), "gradients are float or bfloat16");
@@ -560,7 +570,7 @@ FAST(grad_norm) {
     int rc = abi.norm_query((int)u.item.size(), u.item.data(), &need);
     if (rc) return Py_BuildValue("(i)", rc);
     require(!u.held.empty() || a[2] != Py_None, "no gradients, and no tensor for the result");
-    const at::Tensor out = a[2] != Py_None ? placed(a[2], dev, kWhere) : at::empty({2}, u.held[0].options().dtype(at::kFloat));
+    const at::Tensor out = a[2] != Py_None ? placed(a[2], dev, kWhere) : at::empty({2}, tensor(u.held[0]).options().dtype(at::kFloat));
     require(out.scalar_type() == at::kFloat && out.numel() == 2 && out.is_contiguous(), "out is a contiguous float [2]");
     const at::Tensor ws = scratch_of(a[3], out, need, dev);
     rc = call(abi.norm, (int)u.item.size(), u.item.data(), (float)max_norm, (float*)out.data_ptr(), ws.data_ptr(), (uint64_t)ws.numel(), stream_of(a[5]));
@@ -602,14 +612,10 @@ FAST(adamw_step) {
         it.v_scale = (float*)u.array(a[6], i, at::kFloat, (it.count + 255) / 256, kScale);
       }
       if (masters) {
-        struct Ref { PyObject* o; ~Ref() { Py_XDECREF(o); } } ref{PySequence_GetItem(a[4], i)};
-        if (!ref.o) throw Failed();
-        if (ref.o != Py_None) it.master = (float*)u.array(a[4], i, at::kFloat, it.count, "masters are float (or None), with as many elements as the gradient");
+        if (u.object(a[4], i) != Py_None) it.master = (float*)u.array(a[4], i, at::kFloat, it.count, "masters are float (or None), with as many elements as the gradient");
       }
       if (decays) {
-        struct Ref { PyObject* o; ~Ref() { Py_XDECREF(o); } } ref{PySequence_GetItem(a[7], i)};
-        if (!ref.o) throw Failed();
-        it.weight_decay = (float)number(ref.o);
+        it.weight_decay = (float)number(u.object(a[7], i));
       } else {
         it.weight_decay = (float)decay;
       }

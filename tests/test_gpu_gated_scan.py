@@ -147,7 +147,7 @@ def test_scan_carries_its_state_in_place(T, B, n):
     z = _inputs(2 * T, B, n, "f32", 9, None)[0]
     zt, state = dev(z, "f32"), torch.zeros(B, n, device="cuda")
     y = torch.empty(2 * T, B, n, device="cuda")
-    ws = torch.empty(Bn.gated_scan_query(T, B, n)[1], dtype=torch.uint8, device="cuda")
+    ws = torch.empty(Bn.gated_scan_query(T, B, n)[1] + 1, dtype=torch.uint8, device="cuda")
     for k in range(2):
         part, out = zt[k * T:(k + 1) * T], y[k * T:(k + 1) * T]
         rc = Bn.lib.lstm_gated_scan_fwd(0, 1, T, B, n, part.data_ptr(), 3 * n, state.data_ptr(), None, out.data_ptr(), n, state.data_ptr(), None, 0,
@@ -228,4 +228,6 @@ def test_scan_refuses_what_it_cannot_take():
         with pytest.raises(Bn.LstmError):
             Bn.gated_scan_fwd(z, **bad)
     with pytest.raises(Bn.LstmError):
-        Bn.gated_scan_fwd(z, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+        Bn.gated_scan_fwd(torch.zeros(40000, 1, 24, device="cuda"), workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(Bn.LstmError):
+        Bn.gated_scan_bwd(f, z, torch.zeros(4, 2, 8, device="cuda"), workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))

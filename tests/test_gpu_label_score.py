@@ -225,7 +225,7 @@ def test_refusals():
         with pytest.raises(bad):
             call()
     for call in (lambda: Bn.label_score_fwd(x, l, top=17), lambda: Bn.label_score_fwd(x, l, top=-1),
-                 lambda: Bn.label_score_fwd(x, l, workspace=torch.empty(1, dtype=torch.uint8, device="cuda")),
+                 lambda: Bn.label_score_fwd(torch.zeros(1, 20000, device="cuda"), l[0, :1], workspace=torch.empty(1, dtype=torch.uint8, device="cuda")),
                  lambda: Bn.label_score_bwd(dict(stats=f["stats"], entropy=None), x, l, w, w), lambda: Bn.label_score_bwd(f, x, None, w)):
         with pytest.raises(Bn.LstmError):
             call()
