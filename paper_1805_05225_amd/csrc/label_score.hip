@@ -112,13 +112,14 @@ __device__ __forceinline__ void write_values(const ScoreArgs& a, int r, const T*
 }
 
 // Row r in a.parts stretches, a work-group each (several for few rows, which would leave compute units idle).  A stretch is read once, up to U loads of
-// 16 bytes a thread in flight, and folded four pieces at a time; where alternatives are wanted it stays in registers and they are chosen there as in the beam
+// 16 bytes a thread in flight, and folded a few pieces at a time (two without alternatives, which
+// leaves little of the last round empty: 3200 rows of 20000 bfloat16 values 48 us with four, 36 with two); where alternatives are wanted it stays in registers and they are chosen there as in the beam
 // step: one bound for the whole work-group tells the few entries that can be among the best apart, and these are ranked.  A stretch of more than 64 NW U pieces
 // takes several rounds, each with the best so far among its candidates.
 template <typename T, bool TOP, int U, int NW>
 __global__ __launch_bounds__(64 * NW) void label_score_kernel(ScoreArgs a) {
   typedef Pieces<T> P;
-  constexpr int NT = 64 * NW, E = P::E, G = U < 4 ? U : 4;
+  constexpr int NT = 64 * NW, E = P::E, G = U < 2 ? U : TOP ? (U < 4 ? U : 4) : 2;
   __shared__ Sums part[NW];
   __shared__ typename std::conditional<TOP, Chooser<NW>, int>::type s;
   const int r = (int)blockIdx.x / a.parts, stretch = (int)blockIdx.x - r * a.parts, tid = threadIdx.x;
@@ -158,6 +159,7 @@ __global__ __launch_bounds__(64 * NW) void label_score_kernel(ScoreArgs a) {
     }
 #pragma unroll
     for (int u0 = 0; u0 < U; u0 += G) {
+      if (!TOP && base + u0 * NT >= stop) break;
       float m = sum.m;
 #pragma unroll
       for (int u = u0; u < u0 + G; ++u)
@@ -349,6 +351,15 @@ uint64_t score_bytes(long rows, int parts, int top) {
 }
 template <typename T, bool TOP>
 void launch_rows(const ScoreArgs& a, hipStream_t s) {
+  if constexpr (!TOP) {
+    // Many short rows: a wavefront each, nothing to meet over (4000 rows of 1000 bfloat16 values 11.7 us a call with four, 8.3 with one); few of them
+    // would leave each compute unit a wavefront or two.
+    if (a.parts == 1 && a.step > 64 && a.step <= 512 && (long)a.T * a.B >= 2048) {
+      const auto kernel = a.step <= 128 ? label_score_kernel<T, false, 2, 1> : a.step <= 256 ? label_score_kernel<T, false, 4, 1> : label_score_kernel<T, false, 8, 1>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * a.B)), dim3(64), 0, s, a);
+      return;
+    }
+  }
   const int u = cdiv(a.step, 256);
   const auto row = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * a.B * a.parts)), dim3(64 * waves), 0, s, a); };
   if (a.step <= 64) row(label_score_kernel<T, TOP, 1, 1>, 1);
