@@ -304,8 +304,8 @@ int lstm_embed(int B, int n, int V, const int32_t* label, const void* W_trg, con
  * a search or of generation: feed cT back as c0.
  *   dtype: LSTM_F32 or LSTM_BF16_F32STATE, the type of z, y, dy, dz; states, dc0, dcT, db are float, and so is all arithmetic.
  *   z [T][B][ldz >= 3n]  y [T][B][ldy >= n] (e.g. one half of a wider row)  c0, cT [B][n]: c0 may be NULL (zeros), cT NULL (not wanted) or c0.
- *   reserve: reserve_bytes of lstm_gated_scan_query, written by the forward call for the backward call (the state before every 16th
- *   valid frame, from which the backward call works the others out again); NULL: no backward call follows.
+ *   reserve: reserve_bytes of lstm_gated_scan_query, written by the forward call for the backward call (the state before every 8th
+ *   or 16th valid frame, from which the backward call works the others out again); NULL: no backward call follows.
  * Backward: the exact gradient of sum(dy*y) + sum(dcT*cT), from the forward call's z, seq_lens and reserve, and the same T, B, n, direction.
  *   dy [T][B][lddy >= n]  dcT [B][n] or NULL (zeros)
  *   -> dz [T][B][lddz >= 3n]; dc0 [B][n] or NULL (not wanted); db [3n], the sum of dz over all valid frames before its rounding, or NULL.

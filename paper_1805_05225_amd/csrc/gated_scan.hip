@@ -17,7 +17,11 @@
 namespace lstm {
 namespace {
 
-constexpr int kSeg = 16;              // valid frames between two kept states
+constexpr int kWaves = 8;             // wavefronts of a work-group at most
+// Valid frames of a wavefront in a round, and between two kept states.  16 fill a lane's registers; short batches take 8, so that more wavefronts share
+// them and more of these fit a compute unit (80 frames of 64 rows of 1000 bfloat16 values, backward: 26 us with 16, 20 with 8; 512 of 64 rows of 2048 213 and 219).
+constexpr int kSeg = 16, kSegShort = 8, kShort = 128;
+inline int seg_of(int T) { return T <= kShort ? kSegShort : kSeg; }
 
 // A lane's access: V values of type T in one word, `at` bytes into a row.  A row is a buffer of its own: its address stays in scalar registers, and
 // what lies outside (a lane behind the last unit, a frame that is not there) is read as 0 and not written, without a branch.
@@ -63,7 +67,7 @@ struct ScanArgs {
   const float* c0; const int* lens;
   void* y; long ldy;
   float* cT;
-  float* kept;                        // [ceil(T / kSeg)][B][n]
+  float* kept;                        // [ceil(T / seg_of(T))][B][n]
   const void* dy; long lddy;
   const float* dcT;
   void* dz; long lddz;
@@ -108,10 +112,10 @@ template <typename T> __device__ __forceinline__ Row row_at(const void* base, lo
 // barrier a round is enough.
 template <int V, int NW> struct Chain { float a[2][NW][V][64], c[2][NW][V][64]; };
 
-// The state that enters wavefront `wave`'s frames and the one that leaves all of them, from `state` and the NW compositions.  order: 1 if
+// The state that enters wavefront `wave`'s frames and the one that leaves all of them, from `state` and the compositions of the nw <= NW wavefronts.  order: 1 if
 // wavefront 0 comes first, -1 if it comes last.
 template <int V, int NW>
-__device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wave, int order, const float (&A)[V], const float (&C)[V],
+__device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wave, int nw, int order, const float (&A)[V], const float (&C)[V],
                                      float (&state)[V], float (&mine)[V]) {
   if constexpr (NW == 1) {
 #pragma unroll
@@ -123,6 +127,7 @@ __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wav
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
       const int w = order > 0 ? i : NW - 1 - i;
+      if (w >= nw) continue;
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         if (w == wave) mine[k] = state[k];
@@ -136,10 +141,11 @@ __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wav
 // registers, composes them into one step c -> A c + C, gets the state that enters them from the others' compositions and walks them
 // with it.  So all loads of a round are in flight together, z is read once and only the compositions cross wavefronts.
 template <typename T, int V, int NW, int SEG>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_fwd_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 4) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
-  const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = blockIdx.y, part = a.parts - 1 - (int)blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nw = NW == 1 ? 1 : (int)blockDim.x >> 6;
   const int u = (blockIdx.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_fwd_kerne
         c[k] = fmaf(j.x, c[k], j.y);
       }
   int set = 0;
-  for (int base = sp.begin; base < sp.end; base += NW * SEG, set ^= 1) {
+  for (int base = sp.begin; base < sp.end; base += nw * SEG, set ^= 1) {
     const int s0 = base + wave * SEG, count = min(SEG, sp.end - s0);
     float f[SEG][V], add[SEG][V], A[V], C[V], mine[V];
     unsigned zo[SEG];
@@ -186,11 +192,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_fwd_kerne
         }
       }
     }
-    link<V, NW>(chain, set, lane, wave, 1, A, C, c, mine);
+    link<V, NW>(chain, set, lane, wave, nw, 1, A, C, c, mine);
     if (count > 0) {
       if (a.kept && live) {
 #pragma unroll
-        for (int k = 0; k < V; ++k) a.kept[((long)(s0 / kSeg) * a.B + b) * a.n + u + k] = mine[k];
+        for (int k = 0; k < V; ++k) a.kept[((long)(s0 / SEG) * a.B + b) * a.n + u + k] = mine[k];
       }
       Rows<T> to(a.y, a.ldy, sp, s0, a.n);
 #pragma unroll
@@ -207,7 +213,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_fwd_kerne
   }
   if (!live) return;
   const float zero[V] = {};
-  for (int t = sp.L + part * NW + wave; t < a.T; t += a.parts * NW) W::store(row_at<T>(a.y, (long)t * a.B + b, a.ldy, a.n), o0, zero);
+  for (int t = sp.L + part * nw + wave; t < a.T; t += a.parts * nw) W::store(row_at<T>(a.y, (long)t * a.B + b, a.ldy, a.n), o0, zero);
   if (a.cT && wave == 0 && (sp.L == 0 ? part == 0 : (sp.L - 1) / a.per == part)) {
 #pragma unroll
     for (int k = 0; k < V; ++k) a.cT[(long)b * a.n + u + k] = c[k];
@@ -216,7 +222,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_fwd_kerne
 
 // The compositions of all parts but the last, for the kernel above, and a copy of c0 (which cT may overwrite while other parts read it).
 template <typename T, int V, int NW, int SEG>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_join_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
   const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -273,12 +279,12 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_join_kern
 
 // The same from the other end.  A wavefront works its SEG states out again from the one that the forward pass kept in front of them; what
 // passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.
-template <typename T, int V, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kernel(ScanArgs a) {
+template <typename T, int V, int NW, int SEG>
+__global__ __launch_bounds__(64 * NW, SEG == kSeg ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
-  constexpr int SEG = kSeg;
   __shared__ union { Chain<V, NW> chain; double sum[NW][3][V][64]; } sh;
-  const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = blockIdx.y, part = a.parts - 1 - (int)blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nw = (int)blockDim.x >> 6;
   const int u = (blockIdx.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
@@ -296,8 +302,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kerne
         e[k] = fmaf(j.x, e[k], j.y);
       }
   int set = 0;
-  for (int round = (sp.end - sp.begin + NW * SEG - 1) / (NW * SEG) - 1; round >= 0; --round, set ^= 1) {
-    const int s0 = sp.begin + (round * NW + wave) * SEG, count = min(SEG, sp.end - s0);
+  for (int base = sp.begin + (sp.end - 1 - sp.begin) / (nw * SEG) * (nw * SEG); sp.begin < sp.end && base >= sp.begin; base -= nw * SEG, set ^= 1) {
+    const int s0 = base + wave * SEG, count = min(SEG, sp.end - s0);
     float f[SEG][V], nf[SEG][V], g[SEG][V], o[SEG][V], before[SEG][V], A[V], C[V], mine[V];
     unsigned wy[SEG];
 #pragma unroll
@@ -306,7 +312,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kerne
       unsigned zf[SEG], zg[SEG], zo[SEG];
       float c[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) c[k] = a.kept[((long)(s0 / kSeg) * a.B + b) * a.n + at + k];
+      for (int k = 0; k < V; ++k) c[k] = a.kept[((long)(s0 / SEG) * a.B + b) * a.n + at + k];
       Rows<T> z(a.z, a.ldz, sp, s0, 3 * a.n), dy(a.dy, a.lddy, sp, s0, a.n);
 #pragma unroll
       for (int j = 0; j < SEG; ++j, z.next(), dy.next()) {
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kerne
           C[k] = f[j][k] * fmaf(W::get(wy[j], k), o[j][k], C[k]);
         }
     }
-    link<V, NW>(sh.chain, set, lane, wave, -1, A, C, e, mine);
+    link<V, NW>(sh.chain, set, lane, wave, nw, -1, A, C, e, mine);
     if (count > 0) {
       float sum[3][V] = {};
       Rows<T> to(a.dz, a.lddz, sp, s0 + SEG - 1, 3 * a.n);
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kerne
   }
   if (live) {
     const float zero[V] = {};
-    for (int t = sp.L + part * NW + wave; t < a.T; t += a.parts * NW) {
+    for (int t = sp.L + part * nw + wave; t < a.T; t += a.parts * nw) {
       const Row r = row_at<T>(a.dz, (long)t * a.B + b, a.lddz, 3 * a.n);
       W::store(r, o0, zero);
       W::store(r, o1, zero);
@@ -388,14 +394,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 1) void gated_scan_bwd_kerne
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       double d = 0.0;
-      for (int w = 0; w < NW; ++w) d += sh.sum[w][gate][k][lane];
+      for (int w = 0; w < nw; ++w) d += sh.sum[w][gate][k][lane];
       a.dbpart[(((long)part * a.B + b) * 3 + gate) * a.n + u + k] = d;
     }
 }
 
 // The backward compositions of all parts but the first.
 template <typename T, int V, int NW, int SEG>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void gated_scan_bwd_join_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, 4) void gated_scan_bwd_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
   const int b = blockIdx.y, part = blockIdx.z + 1, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -474,16 +480,15 @@ int scan_dims(int T, int B, int n) {
   if (T < 0 || B < 0 || n < 1 || n > (1 << 27) || B > 65535 || (long)T * B > 0x7fffffffL || (long)B * n > 0x7fffffffL / 3) return LSTM_ERR_DIM;
   return LSTM_OK;
 }
-uint64_t reserve_need(int T, int B, int n) { return (uint64_t)((T + kSeg - 1L) / kSeg) * B * n * 4 + 256; }
+uint64_t reserve_need(int T, int B, int n) { return (uint64_t)cdiv(T, seg_of(T)) * B * n * 4 + 256; }
 
-// How the work is cut.  A wavefront takes 16 frames a round, so short batches have work-groups of fewer wavefronts; where rows and units give
-// too few work-groups for the device, time is cut into parts, whose compositions a launch before works out (a second reading of
-// two thirds of what the forward pass reads, three quarters of the backward pass).
+// How the work is cut.  Short batches have work-groups of fewer wavefronts; where rows and units give too few work-groups for the device, time is cut
+// into parts, whose compositions a launch before works out (a second reading of two thirds of what the forward pass reads, three quarters of the
+// backward pass; it begins with the part that was read last, which the last-level cache still holds).
 struct Cut { int V, waves, parts, per; };
-constexpr int kWaves = 8;
 Cut cut_of(int T, int B, int n, int V) {
   if ((long)cdiv(n, 128) * B < 256) V = 1;                       // twice the work-groups: 2048 frames of 16 rows of 1024 87 -> 69 us forward, 147 -> 109 backward
-  Cut c = {V, T <= kSeg ? 1 : kWaves, 1, std::max(T, 1)};
+  Cut c = {V, std::max(1, std::min(kWaves, cdiv(T, seg_of(T)))), 1, std::max(T, 1)};
   const long groups = (long)cdiv(n, 64 * V) * B;
   constexpr long kGroups = 512;
   const int round = kWaves * kSeg;
@@ -530,8 +535,11 @@ int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
     const auto join = gated_scan_join_kernel<T, V, kWaves, kSeg>;
     hipLaunchKernelGGL(join, most, dim3(64 * kWaves), 0, s, a);
   }
-  const auto kernel = a.T <= 1 ? gated_scan_fwd_kernel<T, V, 1, 1> : c.waves == 1 ? gated_scan_fwd_kernel<T, V, 1, kSeg> : gated_scan_fwd_kernel<T, V, kWaves, kSeg>;
-  hipLaunchKernelGGL(kernel, grid, dim3(64 * c.waves), 0, s, a);
+  // A single work-group a compute unit is twice as wide: 1500 frames of 32 rows of 1024 bfloat16 values 92 us with eight wavefronts, 84 with sixteen.
+  const bool wide = c.waves == kWaves && c.parts == 1 && a.T >= 2 * kWaves * kSeg && (long)grid.x * a.B < 512;
+  const auto kernel = a.T <= 1 ? gated_scan_fwd_kernel<T, V, 1, 1> : a.T <= kShort ? gated_scan_fwd_kernel<T, V, kWaves, kSegShort>
+                      : wide ? gated_scan_fwd_kernel<T, V, 2 * kWaves, kSeg> : gated_scan_fwd_kernel<T, V, kWaves, kSeg>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * (wide ? 2 * kWaves : c.waves)), 0, s, a);
   return status();
 }
 template <typename T, int V>
@@ -541,7 +549,7 @@ int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
     const auto join = gated_scan_bwd_join_kernel<T, V, kWaves, kSeg>;
     hipLaunchKernelGGL(join, most, dim3(64 * kWaves), 0, s, a);
   }
-  const auto kernel = c.waves == 1 ? gated_scan_bwd_kernel<T, V, 1> : gated_scan_bwd_kernel<T, V, kWaves>;
+  const auto kernel = a.T <= kShort ? gated_scan_bwd_kernel<T, V, kWaves, kSegShort> : gated_scan_bwd_kernel<T, V, kWaves, kSeg>;
   if (a.B > 0) hipLaunchKernelGGL(kernel, grid, dim3(64 * c.waves), 0, s, a);
   if (db) hipLaunchKernelGGL(scan_db_kernel, dim3(cdiv(3L * a.n, 64)), dim3(64 * kDbWaves), 0, s, a.dbpart, db, c.parts * a.B, 3 * a.n);
   return status();
