@@ -304,15 +304,14 @@ __global__ __launch_bounds__(64 * NW, SEG == kSeg ? 2 : 4) void gated_scan_bwd_k
   int set = 0;
   for (int base = sp.begin + (sp.end - 1 - sp.begin) / (nw * SEG) * (nw * SEG); sp.begin < sp.end && base >= sp.begin; base -= nw * SEG, set ^= 1) {
     const int s0 = base + wave * SEG, count = min(SEG, sp.end - s0);
-    float f[SEG][V], nf[SEG][V], g[SEG][V], o[SEG][V], before[SEG][V], A[V], C[V], mine[V];
+    float f[SEG][V], nf[SEG][V], g[SEG][V], o[SEG][V], c[SEG + 1][V], A[V], C[V], mine[V];      // c[j], c[j + 1]: the state before and behind frame j
     unsigned wy[SEG];
 #pragma unroll
     for (int k = 0; k < V; ++k) { A[k] = 1.f; C[k] = 0.f; }
     if (count > 0) {
       unsigned zf[SEG], zg[SEG], zo[SEG];
-      float c[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) c[k] = a.kept[((long)(s0 / SEG) * a.B + b) * a.n + at + k];
+      for (int k = 0; k < V; ++k) c[0][k] = a.kept[((long)(s0 / SEG) * a.B + b) * a.n + at + k];
       Rows<T> z(a.z, a.ldz, sp, s0, 3 * a.n), dy(a.dy, a.lddy, sp, s0, a.n);
 #pragma unroll
       for (int j = 0; j < SEG; ++j, z.next(), dy.next()) {
@@ -330,8 +329,7 @@ __global__ __launch_bounds__(64 * NW, SEG == kSeg ? 2 : 4) void gated_scan_bwd_k
           sigmoid_pair(W::get(zf[j], k), f[j][k], nf[j][k]);
           g[j][k] = tanh_(W::get(zg[j], k));
           o[j][k] = sigmoid_(W::get(zo[j], k));
-          before[j][k] = c[k];
-          c[k] = fmaf(f[j][k], c[k], nf[j][k] * g[j][k]);
+          c[j + 1][k] = fmaf(f[j][k], c[j][k], nf[j][k] * g[j][k]);
         }
       }
 #pragma unroll
@@ -351,11 +349,11 @@ __global__ __launch_bounds__(64 * NW, SEG == kSeg ? 2 : 4) void gated_scan_bwd_k
         float df[V], dg[V], dout[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float dy = W::get(wy[j], k), now = fmaf(f[j][k], before[j][k], nf[j][k] * g[j][k]), dc = fmaf(dy, o[j][k], mine[k]);
+          const float dy = W::get(wy[j], k), dc = fmaf(dy, o[j][k], mine[k]);
           mine[k] = f[j][k] * dc;
-          df[k] = (before[j][k] - g[j][k]) * nf[j][k] * mine[k];
+          df[k] = (c[j][k] - g[j][k]) * nf[j][k] * mine[k];
           dg[k] = dc * nf[j][k] * fmaf(-g[j][k], g[j][k], 1.f);
-          dout[k] = dy * now * fmaf(-o[j][k], o[j][k], o[j][k]);
+          dout[k] = dy * c[j + 1][k] * fmaf(-o[j][k], o[j][k], o[j][k]);
           sum[0][k] += df[k]; sum[1][k] += dg[k]; sum[2][k] += dout[k];
         }
         const Row r = to.row(j < count);
