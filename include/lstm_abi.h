@@ -345,7 +345,7 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call; nothing, NULL, where
  *   that is 0); nothing in it has to survive a call.
  * Calls with the same inputs agree bit for bit.
- * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0), LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN,
+ * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0, 2^23 rows or more), LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN,
  * LSTM_ERR_SIZE, LSTM_ERR_HIP. */
 int lstm_label_score_query(int T, int B, int V, int top, uint64_t* workspace_bytes);
 int lstm_label_score_fwd(int dtype, int T, int B, int V, const void* logits, int64_t ld, const int32_t* label, const int32_t* seq_lens,

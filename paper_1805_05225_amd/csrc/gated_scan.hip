@@ -72,7 +72,7 @@ struct ScanArgs {
   const float* dcT;
   void* dz; long lddz;
   float* dc0;
-  double* dbpart;                     // [parts * B][3n]
+  float* dbpart;                      // [parts * B][3n]
   float2* join;                       // [parts][B][n]: what a part's frames do to a state, (factor, addend)
   float* first;                       // [B][n]: copy of c0 or dcT
   int T, B, n, direction;
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(64 * NW, SEG == kSeg ? 2 : 4) void gated_scan_bwd_k
     for (int k = 0; k < V; ++k) {
       double d = 0.0;
       for (int w = 0; w < nw; ++w) d += sh.sum[w][gate][k][lane];
-      a.dbpart[(((long)part * a.B + b) * 3 + gate) * a.n + u + k] = d;
+      a.dbpart[(((long)part * a.B + b) * 3 + gate) * a.n + u + k] = (float)d;
     }
 }
 
@@ -450,14 +450,20 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_bwd_join_kernel(ScanArg
   }
 }
 
-// db = the sum of `rows` rows of partial sums: 64 columns a work-group, whose wavefronts share the rows
+// db = the sum of `rows` rows of partial sums (each added in 64 bits and rounded once): 64 columns a work-group, whose wavefronts share the rows
 constexpr int kDbWaves = 16;
-__global__ __launch_bounds__(64 * kDbWaves) void scan_db_kernel(const double* __restrict__ part, float* __restrict__ db, int rows, int n3) {
+__global__ __launch_bounds__(64 * kDbWaves) void scan_db_kernel(const float* __restrict__ part, float* __restrict__ db, int rows, int n3) {
   __shared__ double sum[kDbWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
   double s = 0.0;
   if (i < n3)
-    for (int r = wave; r < rows; r += kDbWaves) s += part[(long)r * n3 + i];
+    for (int r = wave; r < rows; r += 8 * kDbWaves) {             // eight loads in flight
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = part[(long)min(r + k * kDbWaves, rows - 1) * n3 + i];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += r + k * kDbWaves < rows ? (double)x[k] : 0.0;
+    }
   sum[wave][lane] = s;
   __syncthreads();
   if (wave != 0 || i >= n3) return;
@@ -505,7 +511,7 @@ Places places_of(int T, int B, int n, bool backward) {           // (for either 
   p.join = 0;
   p.first = parts > 1 ? up(parts * state * 2) : 0;
   p.dbpart = p.first + (parts > 1 ? up(state) : 0);
-  p.total = p.dbpart + (backward ? up(parts * state * 6) : 0);
+  p.total = p.dbpart + (backward ? up(parts * state * 3) : 0);
   if (p.total > 0) p.total += 256;
   return p;
 }
@@ -521,7 +527,7 @@ template <typename P> P* aligned(P* p) { return (P*)(((uintptr_t)p + 255) / 256 
 void place(ScanArgs& a, const Cut& c, void* workspace, bool backward) {
   const Places p = places_of(a.T, a.B, a.n, backward);
   char* ws = aligned((char*)workspace);
-  a.join = (float2*)(ws + p.join); a.first = (float*)(ws + p.first); a.dbpart = (double*)(ws + p.dbpart);
+  a.join = (float2*)(ws + p.join); a.first = (float*)(ws + p.first); a.dbpart = (float*)(ws + p.dbpart);
   a.parts = c.parts; a.per = c.per;
 }
 int status() { return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP; }

@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void label_score_bwd_kernel(ScoreArgs a) {
 }
 
 int score_dims(int T, int B, int V, int top) {
-  if (T < 0 || B < 0 || V < 1 || top < 0 || (long)T * B > 0x7fffffffL / 16) return LSTM_ERR_DIM;
+  if (T < 0 || B < 0 || V < 1 || top < 0 || (long)T * B >= 1L << 23) return LSTM_ERR_DIM;
   if (V > kVocabMost || top > kTopMax) return LSTM_ERR_UNSUPPORTED;
   return LSTM_OK;
 }
@@ -443,7 +443,7 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
   a.x = logits; a.ld = ld; a.label = label; a.lens = seq_lens; a.stats_in = (const float2*)stats; a.entropy_in = entropy; a.dlogp = dlogp; a.dent = dent;
   a.dx = dlogits; a.ldd = ldd; a.T = T; a.B = B; a.V = V;
   a.parts = cdiv(V, 256 * kBwdPieces * (dtype == LSTM_F32 ? 4 : 8));
-  if ((long)T * B * a.parts > 0x7fffffffL) return LSTM_ERR_DIM;
+  if ((long)T * B * a.parts >= 1L << 24) return LSTM_ERR_DIM;       // (the threads of a launch)
   hipLaunchKernelGGL(dtype == LSTM_F32 ? label_score_bwd_kernel<float> : label_score_bwd_kernel<bf16_t>, dim3((unsigned)(T * B * a.parts)), dim3(256), 0, (hipStream_t)stream, a);
   return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP;
 }

@@ -371,7 +371,7 @@ int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, floa
   hipStream_t s = (hipStream_t)stream;
   double* part = (double*)(((uintptr_t)workspace + 255) / 256 * 256);
   // tensors of more work-groups than a launch may have are cut into pieces of whole tiles
-  constexpr long kMost = (long)kNormTile << 24;
+  constexpr long kMost = (long)kNormTile << 22;
   NormArgs a;
   a.part = part; a.count = 0;
   unsigned first = 0;
@@ -385,7 +385,7 @@ int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, floa
   const bool few = elements <= kNormFew && count <= kNormItems;
   for (int i = 0; i < count; ++i)
     for (long at = 0; at < items[i].count; at += kMost) {
-      if (a.count == kNormItems || first >= (1u << 24)) flush();
+      if (a.count == kNormItems || first >= (1u << 22)) flush();
       const bool bf16 = items[i].grad_dtype == LSTM_BF16_F32STATE;
       const long n = std::min((long)items[i].count - at, kMost);
       a.item[a.count++] = {(const char*)items[i].grad + at * (bf16 ? 2 : 4), n, first, bf16};
@@ -434,10 +434,10 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
     if (a.count > 0) hipLaunchKernelGGL(eight ? adamw_kernel<true> : adamw_kernel<false>, dim3(first), dim3(256), 0, (hipStream_t)stream, a);
     a.count = 0; first = 0;
   };
-  constexpr long kMost = (long)kTile << 24;
+  constexpr long kMost = (long)kTile << 22;
   for (int i = 0; i < count; ++i)
     for (long at = 0; at < items[i].count; at += kMost) {
-      if (a.count == kItems || first >= (1u << 24)) flush();
+      if (a.count == kItems || first >= (1u << 22)) flush();
       const lstm_adamw_item& it = items[i];
       const bool pb = it.param_dtype == LSTM_BF16_F32STATE, gb = it.grad_dtype == LSTM_BF16_F32STATE;
       const long n = std::min((long)it.count - at, kMost), ss = at * (eight ? 1 : 4);

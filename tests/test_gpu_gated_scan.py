@@ -85,6 +85,13 @@ def test_scan_long(T, B, n, direction, dt):
     _compare(T, B, n, dt, direction, "ragged", seed=8)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,B,n,direction", [(129, 140, 70, 1), (600, 300, 66, -1), (1500, 130, 20, 1)])
+def test_scan_of_many_rows(T, B, n, direction, dt):
+    _compare(T, B, n, dt, direction, "ragged", seed=17)
+    _compare(T, B, n, dt, direction, None, seed=18, state=False)
+
+
 def test_scan_without_state_and_with_odd_lengths():
     _compare(40, 4, 70, "bf16", 1, [-3, 0, 40, 99], state=False)         # lengths are clamped to [0, T]
     _compare(40, 4, 70, "f32", -1, None, state=False)
@@ -141,7 +148,7 @@ def test_scan_two_directions_side_by_side():
     _near("y", y, ref, "bf16")
 
 
-@pytest.mark.parametrize("T,B,n", [(1, 96, 200), (50, 2, 64), (4000, 1, 64)])
+@pytest.mark.parametrize("T,B,n", [(1, 96, 200), (50, 2, 64), (4000, 1, 64), (300, 140, 40)])
 def test_scan_carries_its_state_in_place(T, B, n):
     """cT = c0: the state of a text that arrives in pieces, one array; pieces give what the whole gives."""
     z = _inputs(2 * T, B, n, "f32", 9, None)[0]
@@ -179,8 +186,8 @@ def test_scan_saturated_gates_and_large_values():
     assert torch.equal(h[:, 0, other], f["y"][:, 0, other])
 
 
-def test_scan_repeats_its_bits_on_any_stream_and_in_a_graph():
-    T, B, n = 300, 2, 256
+@pytest.mark.parametrize("T,B,n", [(300, 2, 256), (3000, 2, 64), (500, 130, 64)])
+def test_scan_repeats_its_bits_on_any_stream_and_in_a_graph(T, B, n):
     z, dy, c0, dcT, L = _inputs(T, B, n, "bf16", 4, "ragged")
     zt, dyt, ct, dct, Lt = dev(z, "bf16"), dev(dy, "bf16"), dev(c0), dev(dcT), dev(L)
     run = lambda: (lambda f: (f["y"], f["cT"], *Bn.gated_scan_bwd(f, zt, dyt, Lt, dct).values()))(Bn.gated_scan_fwd(zt, ct, Lt, direction=-1))
