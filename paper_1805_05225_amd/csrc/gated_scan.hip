@@ -35,10 +35,10 @@ template <> struct Word<float, 1> {
   static constexpr unsigned kInf = 0x7f800000u;
 };
 template <> struct Word<bf16_t, 1> {
-  static __device__ unsigned load(Row r, unsigned at) { return (unsigned)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0) << 16; }
-  static __device__ float get(unsigned w, int) { return __uint_as_float(w); }
+  static __device__ unsigned load(Row r, unsigned at) { return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0); }
+  static __device__ float get(unsigned w, int) { return __uint_as_float(w << 16); }      // (not in load, which would wait there)
   static __device__ void store(Row r, unsigned at, const float* v) { __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (bf16_t)v[0]), r, at, 0, 0); }
-  static constexpr unsigned kInf = 0x7f800000u;
+  static constexpr unsigned kInf = 0x7f80u;
 };
 template <> struct Word<bf16_t, 2> {
   typedef __attribute__((ext_vector_type(2))) float f2;
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a)
 // The same from the other end.  A wavefront works its SEG states out again from the one that the forward pass kept in front of them; what
 // passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.
 template <typename T, int V, int NW, int SEG>
-__global__ __launch_bounds__(64 * NW, SEG == kSeg ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ union { Chain<V, NW> chain; double sum[NW][3][V][64]; } sh;
   const int b = blockIdx.y, part = a.parts - 1 - (int)blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
