@@ -654,12 +654,115 @@ def bench_pooled(args, Bn, synth):
     print(json.dumps(out))
 
 
+class LanguageModel:
+    """Gated scan layers, an output layer over V labels, the loss's gradient through all of them, the clipped AdamW step."""
+
+    def __init__(self, Bn, layers, n_in, n, V, T, B, lens):
+        g = torch.Generator(device="cuda").manual_seed(10)
+        rnd = lambda *s: (torch.rand(*s, generator=g, device="cuda") * 2 - 1) * 0.05      # noqa: E731
+        self.Bn, self.n, self.V, self.T, self.B, self.lens = Bn, n, V, T, B, lens
+        self.x = torch.randn(T, B, n_in, generator=g, device="cuda").to(torch.bfloat16)
+        self.labels = torch.randint(0, V, (T, B), generator=g, device="cuda", dtype=torch.int32)
+        self.masters = [rnd(n_in if k == 0 else n, 3 * n) for k in range(layers)] + [rnd(V, n)]
+        self.weights = [w.to(torch.bfloat16) for w in self.masters]
+        self.biases = [torch.zeros(3 * n, device="cuda") for _ in range(layers)] + [torch.zeros(V, device="cuda")]
+        for b in self.biases[:-1]:
+            b[:n] = 2.0                                             # forget gates begin by remembering
+        self.params = self.weights + self.biases
+        self.state = Bn.adamw_state(self.params)
+        self.decay = [0.01] * len(self.weights) + [0.0] * len(self.biases)
+        self.dlogp = torch.full((T, B), -1.0 / int(lens.sum()), device="cuda")
+        self.ones = torch.ones(T * B, 1, dtype=torch.bfloat16, device="cuda")
+        self.count, self.events = 0, None
+
+    def _mark(self, what):
+        if self.events is not None:
+            e = torch.cuda.Event(enable_timing=True)
+            e.record()
+            self.events.append((what, e))
+
+    def step(self):
+        Bn, n, V, T, B, lens = self.Bn, self.n, self.V, self.T, self.B, self.lens
+        F, bf = T * B, torch.bfloat16
+        kept, cur = [], self.x
+        self._mark("start")
+        for W, b in zip(self.weights[:-1], self.biases[:-1]):
+            z = Bn.gemm(cur.view(F, -1), W, a_kcontig=True, b_kcontig=False, M=F, N=3 * n, K=W.shape[0], out_dtype=bf, bias=b).view(T, B, 3 * n)
+            self._mark("products")
+            f = Bn.gated_scan_fwd(z, None, lens, want_state=False)
+            self._mark("scan")
+            kept.append((cur, z, f))
+            cur = f["y"]
+        W, b = self.weights[-1], self.biases[-1]
+        y = cur.view(F, n)
+        logits = Bn.gemm(y, W, a_kcontig=True, b_kcontig=True, M=F, N=V, K=n, out_dtype=bf, bias=b).view(T, B, V)
+        self._mark("products")
+        score = Bn.label_score_fwd(logits, self.labels, lens, want_entropy=False)
+        d = Bn.label_score_bwd(score, logits, self.labels, self.dlogp, None, lens, out=logits).view(F, V)
+        self._mark("loss")
+        dW = [None] * len(self.weights)
+        db = [None] * len(self.biases)
+        dW[-1] = Bn.gemm(d, y, a_kcontig=False, b_kcontig=False, M=V, N=n, K=F)
+        db[-1] = Bn.gemm(self.ones, d, a_kcontig=False, b_kcontig=False, M=1, N=V, K=F).view(V)
+        dy = Bn.gemm(d, W, a_kcontig=True, b_kcontig=False, M=F, N=n, K=V, out_dtype=bf).view(T, B, n)
+        self._mark("products")
+        for k in range(len(kept) - 1, -1, -1):
+            x, z, f = kept[k]
+            g = Bn.gated_scan_bwd(f, z, dy, lens, want_dstate=False)
+            self._mark("scan")
+            W, dz = self.weights[k], g["dz"].view(F, 3 * n)
+            db[k] = g["db"]
+            dW[k] = Bn.gemm(x.view(F, -1), dz, a_kcontig=False, b_kcontig=False, M=W.shape[0], N=3 * n, K=F, lens=lens, Bt=B, T=T)
+            if k > 0:
+                dy = Bn.gemm(dz, W, a_kcontig=True, b_kcontig=True, M=F, N=n, K=3 * n, out_dtype=bf).view(T, B, n)
+            self._mark("products")
+        self.count += 1
+        norm = Bn.grad_norm(dW + db, 1.0)
+        Bn.adamw_step(self.params, dW + db, lr=1e-4, step=self.count, weight_decay=self.decay, grad_scale=norm[1:],
+                      masters=self.masters + [None] * len(self.biases), **self.state)
+        self._mark("update")
+        return score["logp"]
+
+
+def bench_language_model(args, Bn):
+    """--config 10: a training step of a recurrent language model without a product in its loop: 6 gated scan layers (620 -> 1000), 20000 labels."""
+    layers, n_in, n, V, T, B = 6, 620, 1000, 20000, 80, 64
+    lens = torch.randint(20, T + 1, (B,), generator=torch.Generator().manual_seed(10), dtype=torch.int32)
+    lens[0] = T
+    frames = int(lens.sum())
+    m = LanguageModel(Bn, layers, n_in, n, V, T, B, lens.cuda())
+    for _ in range(max(args.warmup, 1)):
+        first = m.step()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(args.steps):
+        last = m.step()
+    torch.cuda.synchronize()
+    dt = time.perf_counter() - t0
+    assert bool(torch.isfinite(last).all()) and bool(torch.isfinite(first).all())
+    m.events = []
+    for _ in range(3):
+        m.step()
+    torch.cuda.synchronize()
+    ms = {}
+    for (_, a), (what, b) in zip(m.events, m.events[1:]):
+        if what != "start":
+            ms[what] = ms.get(what, 0.0) + a.elapsed_time(b) / 3
+    print(json.dumps({
+        "metric": "recurrent language model training frames/sec (n=%d)" % n, "value": frames * args.steps / dt, "unit": "frames/s", "n_gpus": 1,
+        "steps": args.steps, "warmup": args.warmup, "ms_per_step": dt / args.steps * 1e3, "higher_is_better": True, "scaling": "weak",
+        "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
+        "config": {"workload": "config 10: %d gated scan layers, n_in=%d, n=%d, %d labels, B=%d, seq_lens~U{20..%d} (%d real frames), bf16 storage / f32 masters "
+                               "and states, forward + backward + gradient norm + AdamW" % (layers, n_in, n, V, B, T, frames)},
+        "phases_ms_per_step": ms}))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=5)
     ap.add_argument("--warmup", type=int, default=1)
-    ap.add_argument("--config", type=int, default=4, help="synthetic configuration (4 = headline, n = 1024; 2, 3 = other BLSTM stacks; 5 = stepped decoder cell; 6 = config 4 with max-pooling in time between layers; 7 = one bidirectional layer below five unidirectional ones; 8 = decoder step with attention and readout; 9 = complete beam-search step)")
+    ap.add_argument("--config", type=int, default=4, help="synthetic configuration (4 = headline, n = 1024; 2, 3 = other BLSTM stacks; 5 = stepped decoder cell; 6 = config 4 with max-pooling in time between layers; 7 = one bidirectional layer below five unidirectional ones; 8 = decoder step with attention and readout; 9 = complete beam-search step; 10 = training step of a language model of gated scans)")
     ap.add_argument("--no-cpu", action="store_true", help="skip the CPU oracle baseline")
     ap.add_argument("--per-step", action="store_true", help="force one launch per time step")
     ap.add_argument("--copy-calibration", action="store_true",
@@ -691,6 +794,9 @@ def main():
         return
     if args.config == 9:
         bench_search_step(args, Bn, synth)
+        return
+    if args.config == 10:
+        bench_language_model(args, Bn)
         return
     inp = synth.make(args.config)
     cfg = inp["cfg"]
