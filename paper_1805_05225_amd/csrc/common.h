@@ -479,6 +479,8 @@ inline size_t frag_bytes(long rows, long K) { return (size_t)((rows + 15) / 16) 
 hipError_t launch_cell_step(const float* z, long part, int nparts, const float* bias, const float* h_in, const float* c_in, float* h_out,
                             float* c_out, void* y, long ldy, float* cs, const int* lens, unsigned* status, int B, int n, int ndir, hipStream_t s);
 
+// Passes over more memory than the last-level cache holds read it past the caches: what they would leave there is gone before anyone comes back for it.
+constexpr uint64_t kLastLevelBytes = 256ull << 20;
 inline int cdiv(long a, long b) { return (int)((a + b - 1) / b); }
 
 // Do two arrays of `rows` rows share a byte?  Row strides and widths in bytes; column blocks of one matrix (same stride) do not.

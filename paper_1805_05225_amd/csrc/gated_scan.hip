@@ -27,15 +27,16 @@ inline int seg_of(int T) { return T <= kShort ? kSegShort : kSeg; }
 // what lies outside (a lane behind the last unit, a frame that is not there) is read as 0 and not written, without a branch.
 typedef __amdgpu_buffer_rsrc_t Row;
 constexpr unsigned kOutside = 0x80000000u;
+constexpr int kNonTemporal = 2;         // cache policy of a load: past the caches
 template <typename T, int V> struct Word;
 template <> struct Word<float, 1> {
-  static __device__ unsigned load(Row r, unsigned at) { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0); }
+  template <int POLICY> static __device__ unsigned load(Row r, unsigned at) { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, POLICY); }
   static __device__ float get(unsigned w, int) { return __uint_as_float(w); }
   static __device__ void store(Row r, unsigned at, const float* v) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[0]), r, at, 0, 0); }
   static constexpr unsigned kInf = 0x7f800000u;
 };
 template <> struct Word<bf16_t, 1> {
-  static __device__ unsigned load(Row r, unsigned at) { return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0); }
+  template <int POLICY> static __device__ unsigned load(Row r, unsigned at) { return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, at, 0, POLICY); }
   static __device__ float get(unsigned w, int) { return __uint_as_float(w << 16); }      // (not in load, which would wait there)
   static __device__ void store(Row r, unsigned at, const float* v) { __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (bf16_t)v[0]), r, at, 0, 0); }
   static constexpr unsigned kInf = 0x7f80u;
@@ -43,7 +44,7 @@ template <> struct Word<bf16_t, 1> {
 template <> struct Word<bf16_t, 2> {
   typedef __attribute__((ext_vector_type(2))) float f2;
   typedef __attribute__((ext_vector_type(2))) bf16_t b2;
-  static __device__ unsigned load(Row r, unsigned at) { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0); }
+  template <int POLICY> static __device__ unsigned load(Row r, unsigned at) { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, POLICY); }
   static __device__ float get(unsigned w, int k) { return __uint_as_float(k == 0 ? w << 16 : w & 0xffff0000u); }
   static __device__ void store(Row r, unsigned at, const float* v) {        // rounded to nearest, ties to even
     const f2 x = {v[0], v[1]};
@@ -140,7 +141,7 @@ __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wav
 // A work-group takes 64 V units of one row of the batch through a part of time, NW * SEG frames a round: every wavefront has SEG of them in
 // registers, composes them into one step c -> A c + C, gets the state that enters them from the others' compositions and walks them
 // with it.  So all loads of a round are in flight together, z is read once and only the compositions cross wavefronts.
-template <typename T, int V, int NW, int SEG>
+template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 4) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
@@ -175,9 +176,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 4) void gated_scan_fwd_kerne
 #pragma unroll
       for (int j = 0; j < SEG; ++j, z.next()) {
         const Row r = z.row(j < count);
-        zf[j] = W::load(r, o0);
-        zg[j] = W::load(r, o1);
-        zo[j] = W::load(r, o2);
+        zf[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o0);
+        zg[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o1);
+        zo[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o2);
       }
 #pragma unroll
       for (int j = 0; j < SEG; ++j) {
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 4) void gated_scan_fwd_kerne
 }
 
 // The compositions of all parts but the last, for the kernel above, and a copy of c0 (which cT may overwrite while other parts read it).
-template <typename T, int V, int NW, int SEG>
+template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
@@ -247,8 +248,8 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a)
 #pragma unroll
     for (int j = 0; j < SEG; ++j, z.next()) {
       const Row r = z.row(j < count);
-      zf[j] = W::load(r, o0);
-      zg[j] = W::load(r, o1);
+      zf[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o0);
+      zg[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o1);
     }
 #pragma unroll
     for (int j = 0; j < SEG; ++j) {
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a)
 
 // The same from the other end.  A wavefront works its SEG states out again from the one that the forward pass kept in front of them; what
 // passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.
-template <typename T, int V, int NW, int SEG>
+template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ union { Chain<V, NW> chain; double sum[NW][3][V][64]; } sh;
@@ -316,10 +317,10 @@ __global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) voi
 #pragma unroll
       for (int j = 0; j < SEG; ++j, z.next(), dy.next()) {
         const Row r = z.row(j < count);
-        zf[j] = W::load(r, o0);
-        zg[j] = W::load(r, o1);
-        zo[j] = W::load(r, o2);
-        wy[j] = W::load(dy.row(j < count), o0);
+        zf[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o0);
+        zg[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o1);
+        zo[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o2);
+        wy[j] = W::template load<STREAM ? kNonTemporal : 0>(dy.row(j < count), o0);
       }
 #pragma unroll
       for (int j = 0; j < SEG; ++j) {
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) voi
 }
 
 // The backward compositions of all parts but the first.
-template <typename T, int V, int NW, int SEG>
+template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_bwd_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
@@ -420,9 +421,9 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_bwd_join_kernel(ScanArg
 #pragma unroll
     for (int j = 0; j < SEG; ++j, z.next(), dy.next()) {
       const Row r = z.row(j < count);
-      zf[j] = W::load(r, o0);
-      zo[j] = W::load(r, o2);
-      wy[j] = W::load(dy.row(j < count), o0);
+      zf[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o0);
+      zo[j] = W::template load<STREAM ? kNonTemporal : 0>(r, o2);
+      wy[j] = W::template load<STREAM ? kNonTemporal : 0>(dy.row(j < count), o0);
     }
 #pragma unroll
     for (int j = SEG - 1; j >= 0; --j) {
@@ -532,31 +533,40 @@ void place(ScanArgs& a, const Cut& c, void* workspace, bool backward) {
 }
 int status() { return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP; }
 
-template <typename T, int V>
+// STREAM: a call that moves more than the last-level cache holds (us, 32768 x 1 x 1024 float 167 -> 153 forward and 275 -> 261 backward, 512 x 64 x 2048 bfloat16 121 -> 110
+// forward, 1500 x 32 x 1024 141 -> 125 backward; 80 x 64 x 1000, which fits, 19 -> 23 backward).
+template <typename T, int V, bool STREAM>
 int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
   const dim3 grid(cdiv(a.n, 64 * V), a.B, c.parts), most(grid.x, grid.y, c.parts - 1);
   if (c.parts > 1) {
-    const auto join = gated_scan_join_kernel<T, V, kWaves, kSeg>;
+    const auto join = gated_scan_join_kernel<T, V, kWaves, kSeg, STREAM>;
     hipLaunchKernelGGL(join, most, dim3(64 * kWaves), 0, s, a);
   }
   // A single work-group a compute unit is twice as wide: 1500 frames of 32 rows of 1024 bfloat16 values 92 us with eight wavefronts, 84 with sixteen.
   const bool wide = c.waves == kWaves && c.parts == 1 && a.T >= 2 * kWaves * kSeg && (long)grid.x * a.B < 512;
-  const auto kernel = a.T <= 1 ? gated_scan_fwd_kernel<T, V, 1, 1> : a.T <= kShort ? gated_scan_fwd_kernel<T, V, kWaves, kSegShort>
-                      : wide ? gated_scan_fwd_kernel<T, V, 2 * kWaves, kSeg> : gated_scan_fwd_kernel<T, V, kWaves, kSeg>;
+  const auto kernel = a.T <= 1 ? gated_scan_fwd_kernel<T, V, 1, 1, STREAM> : a.T <= kShort ? gated_scan_fwd_kernel<T, V, kWaves, kSegShort, STREAM>
+                      : wide ? gated_scan_fwd_kernel<T, V, 2 * kWaves, kSeg, STREAM> : gated_scan_fwd_kernel<T, V, kWaves, kSeg, STREAM>;
   hipLaunchKernelGGL(kernel, grid, dim3(64 * (wide ? 2 * kWaves : c.waves)), 0, s, a);
   return status();
 }
-template <typename T, int V>
+template <typename T, int V, bool STREAM>
 int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
   const dim3 grid(cdiv(a.n, 64 * V), a.B, c.parts), most(grid.x, grid.y, c.parts - 1);
   if (c.parts > 1) {
-    const auto join = gated_scan_bwd_join_kernel<T, V, kWaves, kSeg>;
+    const auto join = gated_scan_bwd_join_kernel<T, V, kWaves, kSeg, STREAM>;
     hipLaunchKernelGGL(join, most, dim3(64 * kWaves), 0, s, a);
   }
-  const auto kernel = a.T <= kShort ? gated_scan_bwd_kernel<T, V, kWaves, kSegShort> : gated_scan_bwd_kernel<T, V, kWaves, kSeg>;
+  const auto kernel = a.T <= kShort ? gated_scan_bwd_kernel<T, V, kWaves, kSegShort, STREAM> : gated_scan_bwd_kernel<T, V, kWaves, kSeg, STREAM>;
   if (a.B > 0) hipLaunchKernelGGL(kernel, grid, dim3(64 * c.waves), 0, s, a);
   if (db) hipLaunchKernelGGL(scan_db_kernel, dim3(cdiv(3L * a.n, 64)), dim3(64 * kDbWaves), 0, s, a.dbpart, db, c.parts * a.B, 3 * a.n);
   return status();
+}
+bool streams(const ScanArgs& a, int size, int values) { return (uint64_t)a.T * a.B * a.n * size * values > kLastLevelBytes; }      // values: a unit's, of a frame
+template <typename T, int V>
+int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) { return streams(a, sizeof(T), 4) ? run_fwd<T, V, true>(a, c, s) : run_fwd<T, V, false>(a, c, s); }
+template <typename T, int V>
+int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
+  return streams(a, sizeof(T), 7) ? run_bwd<T, V, true>(a, c, db, s) : run_bwd<T, V, false>(a, c, db, s);
 }
 
 }  // namespace

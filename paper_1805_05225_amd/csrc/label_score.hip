@@ -116,7 +116,7 @@ __device__ __forceinline__ void write_values(const ScoreArgs& a, int r, const T*
 // leaves little of the last round empty: 3200 rows of 20000 bfloat16 values 48 us with four, 36 with two); where alternatives are wanted it stays in registers and they are chosen there as in the beam
 // step: one bound for the whole work-group tells the few entries that can be among the best apart, and these are ranked.  A stretch of more than 64 NW U pieces
 // takes several rounds, each with the best so far among its candidates.
-template <typename T, bool TOP, int U, int NW>
+template <typename T, bool TOP, int U, int NW, bool STREAM = false>
 __global__ __launch_bounds__(64 * NW) void label_score_kernel(ScoreArgs a) {
   typedef Pieces<T> P;
   constexpr int NT = 64 * NW, E = P::E, G = U < 2 ? U : TOP ? (U < 4 ? U : 4) : 2;
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * NW) void label_score_kernel(ScoreArgs a) {
     const int stop = min(end, base + a.step);
     u32x4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = __builtin_amdgcn_raw_buffer_load_b128(rs, (unsigned)(base + u * NT + tid) * 16u, 0, 0);
+    for (int u = 0; u < U; ++u) w[u] = __builtin_amdgcn_raw_buffer_load_b128(rs, (unsigned)(base + u * NT + tid) * 16u, 0, STREAM ? 2 : 0);      // (2: non-temporal)
     if (base + U * NT > stop) {       // pieces behind the end hold -inf
       const int left = stop - base - tid;
 #pragma unroll
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(64) void label_score_merge_kernel(ScoreArgs a) {
 // dlogits: a work-group takes up to kBwdPieces pieces a thread of one row, read and written once.  Rows of logits and of dlogits that lie differently to the
 // 16-byte boundaries go value by value.
 constexpr int kBwdPieces = 4;
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void label_score_bwd_kernel(ScoreArgs a) {
   typedef Pieces<T> P;
   constexpr int E = P::E;
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(256) void label_score_bwd_kernel(ScoreArgs a) {
   for (int u = 0; u < kBwdPieces; ++u) {
     const int p = begin + u * 256 + tid;
     w[u] = u32x4{0u, 0u, 0u, 0u};
-    if (!none && p < at.pieces) w[u] = from[p];
+    if (!none && p < at.pieces) w[u] = STREAM ? __builtin_nontemporal_load(from + p) : from[p];
   }
   if (stretch == 0 && tid < at.head + at.tail) {
     const int v = at.outside(tid);
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(256) void label_score_bwd_kernel(ScoreArgs a) {
         }
       }
     }
-    to[p] = w[u];
+    if (STREAM) __builtin_nontemporal_store(w[u], to + p); else to[p] = w[u];
   }
 }
 
@@ -349,6 +349,9 @@ uint64_t whole(uint64_t b) { return (b + 255) / 256 * 256; }
 uint64_t score_bytes(long rows, int parts, int top) {
   return parts == 1 ? 0 : 256 + whole((uint64_t)rows * parts * sizeof(float4)) + 2 * whole((uint64_t)rows * parts * top * 4);
 }
+// Logits that the last-level cache does not hold (us: 2048 rows of 131071 float 204 -> 198 forward, 383 -> 372 backward; 5120 of 20000 152 -> 131 backward; 64 of 131071,
+// which fit, 12 -> 15).
+template <typename T> bool streams(const ScoreArgs& a) { return (uint64_t)a.T * a.B * a.V * sizeof(T) > kLastLevelBytes; }
 template <typename T, bool TOP>
 void launch_rows(const ScoreArgs& a, hipStream_t s) {
   if constexpr (!TOP) {
@@ -368,6 +371,7 @@ void launch_rows(const ScoreArgs& a, hipStream_t s) {
   else if (u <= 4) row(label_score_kernel<T, TOP, 4, 4>, 4);
   else if (u <= 8) row(label_score_kernel<T, TOP, 8, 4>, 4);
   else if (u <= 12) row(label_score_kernel<T, TOP, 12, 4>, 4);
+  else if (!TOP && streams<T>(a)) row(label_score_kernel<T, false, 16, 4, true>, 4);
   else if (!TOP || u <= 16) row(label_score_kernel<T, TOP, 16, 4>, 4);
   else if constexpr (TOP) row(u <= 20 ? label_score_kernel<T, TOP, 20, 4> : label_score_kernel<T, TOP, kPieces, 4>, 4);
 }
@@ -444,7 +448,9 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
   a.dx = dlogits; a.ldd = ldd; a.T = T; a.B = B; a.V = V;
   a.parts = cdiv(V, 256 * kBwdPieces * (dtype == LSTM_F32 ? 4 : 8));
   if ((long)T * B * a.parts >= 1L << 24) return LSTM_ERR_DIM;       // (the threads of a launch)
-  hipLaunchKernelGGL(dtype == LSTM_F32 ? label_score_bwd_kernel<float> : label_score_bwd_kernel<bf16_t>, dim3((unsigned)(T * B * a.parts)), dim3(256), 0, (hipStream_t)stream, a);
+  const auto kernel = dtype == LSTM_F32 ? (streams<float>(a) ? label_score_bwd_kernel<float, true> : label_score_bwd_kernel<float, false>)
+                                        : (streams<bf16_t>(a) ? label_score_bwd_kernel<bf16_t, true> : label_score_bwd_kernel<bf16_t, false>);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(T * B * a.parts)), dim3(256), 0, (hipStream_t)stream, a);
   return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP;
 }
 
