@@ -101,7 +101,8 @@ __device__ __forceinline__ Sums join_all(Sums s, Sums* part) {                  
 template <typename T>
 __device__ __forceinline__ void write_values(const ScoreArgs& a, int r, const T* row, const Sums& s, float logz) {      // by one thread
   const bool pad = padded(a, r), empty = s.z == 0.f;
-  if (a.stats) a.stats[r] = pad ? make_float2(0.f, 0.f) : empty ? make_float2(-__builtin_inff(), 0.f) : make_float2(s.m, logz);
+  const float m = s.z != s.z ? s.z : s.m;                        // (a row of NaN has no maximum, and is not an empty one)
+  if (a.stats) a.stats[r] = pad ? make_float2(0.f, 0.f) : empty ? make_float2(-__builtin_inff(), 0.f) : make_float2(m, logz);
   if (a.entropy) a.entropy[r] = pad || empty ? 0.f : logz - kLn2 * (s.u / s.z);
   if (a.logp) {
     const int l = a.label[r];

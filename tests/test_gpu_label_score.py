@@ -149,6 +149,28 @@ def test_rows_with_nothing_and_rows_with_too_much(V, dt):
     assert np.allclose(d[0][finite], do[0][finite], rtol=2.0 ** -8 if dt == "bf16" else 1e-4, atol=1e-4)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [9, 30000])
+def test_rows_of_nan_alone(V, dt):
+    """No maximum to be found: values and gradient are NaN all the same, not those of a row where nothing can occur."""
+    x = np.full((1, 3, V), np.nan, dtype=np.float32)
+    x[0, 1, ::2] = -np.inf
+    x[0, 2] = -np.inf
+    label, w = torch.zeros(1, 3, dtype=torch.int32, device="cuda"), torch.ones(1, 3, device="cuda")
+    f = Bn.label_score_fwd(dev(x, dt), label, top=2)
+    d = Bn.label_score_bwd(f, dev(x, dt), label, w, w)
+    for k in ("logp", "entropy"):
+        assert torch.isnan(f[k][0, :2]).all()
+    assert torch.isnan(f["stats"][0, :2]).all() and torch.isnan(d[0, :2]).all()
+    assert f["logp"][0, 2] == -np.inf and f["entropy"][0, 2] == 0 and not d[0, 2].any()
+    assert (f["top_logp"] == -np.inf).all() and not f["top_label"].any()
+
+
+def test_more_alternatives_than_labels():
+    rng, x, label = _case(2, 3, 5, 2)
+    _check(x, label, "f32", None, 16, None, None)
+
+
 def test_large_logits():
     rng, x, label = _case(1, 8, 5000, 3, spread=2000.0)
     _check(x, label, "f32", None, 8, np.ones((1, 8), np.float32), None)
