@@ -53,6 +53,12 @@ template <> struct Word<bf16_t, 2> {
   static constexpr unsigned kInf = 0x7f807f80u;
 };
 
+// The same behind an address of the lane's own.
+template <typename T, int V> __device__ __forceinline__ unsigned word_at(const void* p, long i) {
+  if constexpr (sizeof(T) * V == 4) return *(const unsigned*)((const T*)p + i);
+  else return *((const uint16_t*)p + i);
+}
+
 // sigmoid(x) and 1 - sigmoid(x) with e = exp(-x): 1 / (1 + e) and e / (1 + e), each with a float's relative accuracy (1 - f has few bits left
 // where a forget gate is near 1).  Where e is infinite the second is inf * 0 and becomes 1; a NaN stays in the first.
 __device__ __forceinline__ void sigmoid_pair(float x, float& s, float& not_s) {
@@ -118,22 +124,17 @@ template <int V, int NW> struct Chain { float a[2][NW][V][64], c[2][NW][V][64]; 
 template <int V, int NW>
 __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wave, int nw, int order, const float (&A)[V], const float (&C)[V],
                                      float (&state)[V], float (&mine)[V]) {
-  if constexpr (NW == 1) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) { mine[k] = state[k]; state[k] = fmaf(A[k], state[k], C[k]); }
-  } else {
+  for (int k = 0; k < V; ++k) { s.a[set][wave][k][lane] = A[k]; s.c[set][wave][k][lane] = C[k]; }
+  __syncthreads();
 #pragma unroll
-    for (int k = 0; k < V; ++k) { s.a[set][wave][k][lane] = A[k]; s.c[set][wave][k][lane] = C[k]; }
-    __syncthreads();
+  for (int i = 0; i < NW; ++i) {
+    const int w = order > 0 ? i : NW - 1 - i;
+    if (w >= nw) continue;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-      const int w = order > 0 ? i : NW - 1 - i;
-      if (w >= nw) continue;
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        if (w == wave) mine[k] = state[k];
-        state[k] = fmaf(s.a[set][w][k][lane], state[k], s.c[set][w][k][lane]);
-      }
+    for (int k = 0; k < V; ++k) {
+      if (w == wave) mine[k] = state[k];
+      state[k] = fmaf(s.a[set][w][k][lane], state[k], s.c[set][w][k][lane]);
     }
   }
 }
@@ -142,11 +143,11 @@ __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wav
 // registers, composes them into one step c -> A c + C, gets the state that enters them from the others' compositions and walks them
 // with it.  So all loads of a round are in flight together, z is read once and only the compositions cross wavefronts.
 template <typename T, int V, int NW, int SEG, bool STREAM>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 4) void gated_scan_fwd_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, 4) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
   const int b = blockIdx.y, part = a.parts - 1 - (int)blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int nw = NW == 1 ? 1 : (int)blockDim.x >> 6;
+  const int nw = (int)blockDim.x >> 6;
   const int u = (blockIdx.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
@@ -218,6 +219,40 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 4) void gated_scan_fwd_kerne
   if (a.cT && wave == 0 && (sp.L == 0 ? part == 0 : (sp.L - 1) / a.per == part)) {
 #pragma unroll
     for (int k = 0; k < V; ++k) a.cT[(long)b * a.n + u + k] = c[k];
+  }
+}
+
+// One frame (or none), the step of a search or of generation: nothing to compose, a lane per word of any row.  (As a stretch of one frame of the kernel above,
+// a wavefront per row and 64 words: 768 rows of 1000 bfloat16 values 6.2 us, 4.4 so.)
+template <typename T, int V>
+__global__ __launch_bounds__(256) void gated_scan_step_kernel(ScanArgs a) {
+  typedef Word<T, V> W;
+  const unsigned i = blockIdx.x * 256 + threadIdx.x, per_row = (unsigned)(a.n / V);
+  if (i >= per_row * (unsigned)a.B) return;
+  const int b = (int)(i / per_row), u = (int)(i - (unsigned)b * per_row) * V;
+  const long state = (long)b * a.n + u, row = (long)b * a.ldz + u;
+  float c[V], y[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) c[k] = a.c0 ? a.c0[state + k] : 0.f;
+  const bool valid = a.T > 0 && (!a.lens || a.lens[b] > 0);
+  if (valid) {
+    const unsigned zf = word_at<T, V>(a.z, row), zg = word_at<T, V>(a.z, row + a.n), zo = word_at<T, V>(a.z, row + 2L * a.n);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      if (a.kept) a.kept[state + k] = c[k];
+      float f, nf;
+      sigmoid_pair(W::get(zf, k), f, nf);
+      c[k] = fmaf(f, c[k], nf * tanh_(W::get(zg, k)));
+      y[k] = sigmoid_(W::get(zo, k)) * c[k];
+    }
+  }
+  if (a.T > 0) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) ((T*)a.y)[(long)b * a.ldy + u + k] = (T)(valid ? y[k] : 0.f);
+  }
+  if (a.cT) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) a.cT[state + k] = c[k];
   }
 }
 
@@ -492,7 +527,7 @@ uint64_t reserve_need(int T, int B, int n) { return (uint64_t)cdiv(T, seg_of(T))
 // backward pass; it begins with the part that was read last, which the last-level cache still holds).
 struct Cut { int V, waves, parts, per; };
 Cut cut_of(int T, int B, int n, int V) {
-  if ((long)cdiv(n, 128) * B < 256) V = 1;                       // twice the work-groups: 2048 frames of 16 rows of 1024 87 -> 69 us forward, 147 -> 109 backward
+  if (T > 1 && (long)cdiv(n, 128) * B < 256) V = 1;                       // twice the work-groups: 2048 frames of 16 rows of 1024 87 -> 69 us forward, 147 -> 109 backward
   Cut c = {V, std::max(1, std::min(kWaves, cdiv(T, seg_of(T)))), 1, std::max(T, 1)};
   const long groups = (long)cdiv(n, 64 * V) * B;
   constexpr long kGroups = 512;
@@ -544,7 +579,7 @@ int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
   }
   // A single work-group a compute unit is twice as wide: 1500 frames of 32 rows of 1024 bfloat16 values 92 us with eight wavefronts, 84 with sixteen.
   const bool wide = c.waves == kWaves && c.parts == 1 && a.T >= 2 * kWaves * kSeg && (long)grid.x * a.B < 512;
-  const auto kernel = a.T <= 1 ? gated_scan_fwd_kernel<T, V, 1, 1, STREAM> : a.T <= kShort ? gated_scan_fwd_kernel<T, V, kWaves, kSegShort, STREAM>
+  const auto kernel = a.T <= kShort ? gated_scan_fwd_kernel<T, V, kWaves, kSegShort, STREAM>
                       : wide ? gated_scan_fwd_kernel<T, V, 2 * kWaves, kSeg, STREAM> : gated_scan_fwd_kernel<T, V, kWaves, kSeg, STREAM>;
   hipLaunchKernelGGL(kernel, grid, dim3(64 * (wide ? 2 * kWaves : c.waves)), 0, s, a);
   return status();
@@ -563,7 +598,13 @@ int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
 }
 bool streams(const ScanArgs& a, int size, int values) { return (uint64_t)a.T * a.B * a.n * size * values > kLastLevelBytes; }      // values: a unit's, of a frame
 template <typename T, int V>
-int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) { return streams(a, sizeof(T), 4) ? run_fwd<T, V, true>(a, c, s) : run_fwd<T, V, false>(a, c, s); }
+int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
+  if (a.T <= 1) {
+    hipLaunchKernelGGL((gated_scan_step_kernel<T, V>), dim3(cdiv((long)(a.n / V) * a.B, 256)), dim3(256), 0, s, a);
+    return status();
+  }
+  return streams(a, sizeof(T), 4) ? run_fwd<T, V, true>(a, c, s) : run_fwd<T, V, false>(a, c, s);
+}
 template <typename T, int V>
 int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
   return streams(a, sizeof(T), 7) ? run_bwd<T, V, true>(a, c, db, s) : run_bwd<T, V, false>(a, c, db, s);
