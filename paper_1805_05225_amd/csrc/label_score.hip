@@ -22,6 +22,8 @@ constexpr int kVocabMost = 1 << 26;
 constexpr int kPieces = 24;           // 16-byte pieces of a row that a thread holds at most where they are kept
 constexpr int kStretches = 32;        // stretches of a row at most
 constexpr long kStretchGroups = 768;  // work-groups up to which rows are cut into stretches
+constexpr long kWholeRows = 256;      // rows, and labels of a row, whose alternatives sixteen wavefronts choose in one launch
+constexpr int kWholeFrom = 4096, kWholeTo = 32768;
 
 typedef __attribute__((ext_vector_type(2))) float f32x2_;
 typedef __attribute__((ext_vector_type(2))) bf16_t bf16x2_;
@@ -120,7 +122,8 @@ __device__ __forceinline__ void write_values(const ScoreArgs& a, int r, const T*
 template <typename T, bool TOP, int U, int NW, bool STREAM = false>
 __global__ __launch_bounds__(64 * NW) void label_score_kernel(ScoreArgs a) {
   typedef Pieces<T> P;
-  constexpr int NT = 64 * NW, E = P::E, G = U < 2 ? U : TOP ? (U < 4 ? U : 4) : 2;
+  constexpr int NT = 64 * NW, E = P::E, G = U < 2 ? U : TOP && U % 4 == 0 ? 4 : 2;
+  static_assert(U % G == 0, "pieces are folded G at a time");
   __shared__ Sums part[NW];
   __shared__ typename std::conditional<TOP, Chooser<NW>, int>::type s;
   const int r = (int)blockIdx.x / a.parts, stretch = (int)blockIdx.x - r * a.parts, tid = threadIdx.x;
@@ -344,8 +347,13 @@ int score_dims(int T, int B, int V, int top) {
   if (V > kVocabMost || top > kTopMax) return LSTM_ERR_UNSUPPORTED;
   return LSTM_OK;
 }
+// Alternatives of few rows that sixteen wavefronts hold at once, a row a compute unit: one launch instead of stretches and their merge (8 alternatives, us in a replayed
+// graph: 1 row of 5000 float 7.3 against 8.3, 1 of 20000 8.6 both, 100 of 20000 9.4 against 11.3, and 3 us less on
+// the host; 400 rows, two a compute unit, 19.8 against 12.3). Scores alone
+// are read faster than the wider meeting ends (1 row of 20000 6.1 against 5.2).
+bool whole_rows(long rows, int V, int top) { return top > 0 && rows <= kWholeRows && V > kWholeFrom && V <= kWholeTo; }
 // Stretches a row is cut into: as many as the device holds at once (three work-groups a compute unit), of at least 2048 entries.
-int stretches(long rows, int V) { return rows < 1 ? 1 : (int)std::max(1L, std::min({(long)kStretches, kStretchGroups / rows, (long)V / 2048})); }
+int stretches(long rows, int V, int top) { return rows < 1 || whole_rows(rows, V, top) ? 1 : (int)std::max(1L, std::min({(long)kStretches, kStretchGroups / rows, (long)V / 2048})); }
 uint64_t whole(uint64_t b) { return (b + 255) / 256 * 256; }
 uint64_t score_bytes(long rows, int parts, int top) {
   return parts == 1 ? 0 : 256 + whole((uint64_t)rows * parts * sizeof(float4)) + 2 * whole((uint64_t)rows * parts * top * 4);
@@ -354,13 +362,23 @@ uint64_t score_bytes(long rows, int parts, int top) {
 // which fit, 12 -> 15).
 template <typename T> bool streams(const ScoreArgs& a) { return (uint64_t)a.T * a.B * a.V * sizeof(T) > kLastLevelBytes; }
 template <typename T, bool TOP>
-void launch_rows(const ScoreArgs& a, hipStream_t s) {
+void launch_rows(ScoreArgs a, hipStream_t s) {
   if constexpr (!TOP) {
     // Many short rows: a wavefront each, nothing to meet over (4000 rows of 1000 bfloat16 values 11.7 us a call with four, 8.3 with one); few of them
     // would leave each compute unit a wavefront or two.
     if (a.parts == 1 && a.step > 64 && a.step <= 512 && (long)a.T * a.B >= 2048) {
       const auto kernel = a.step <= 128 ? label_score_kernel<T, false, 2, 1> : a.step <= 256 ? label_score_kernel<T, false, 4, 1> : label_score_kernel<T, false, 8, 1>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * a.B)), dim3(64), 0, s, a);
+      return;
+    }
+  }
+  if constexpr (TOP) {
+    if (whole_rows((long)a.T * a.B, a.V, a.top)) {
+      a.step = a.per;                                           // (one round: at most 8 pieces a thread of float, 4 of bfloat16)
+      const int w = cdiv(a.per, 1024);
+      auto kernel = w <= 2 ? label_score_kernel<T, true, 2, 16> : label_score_kernel<T, true, 4, 16>;
+      if constexpr (Pieces<T>::E == 4) kernel = w <= 4 ? kernel : w <= 6 ? label_score_kernel<T, true, 6, 16> : label_score_kernel<T, true, 8, 16>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * a.B)), dim3(1024), 0, s, a);
       return;
     }
   }
@@ -399,7 +417,7 @@ int lstm_label_score_query(int T, int B, int V, int top, uint64_t* workspace_byt
   if (!workspace_bytes) return LSTM_ERR_NULL;
   const int rc = score_dims(T, B, V, top);
   if (rc) return rc;
-  *workspace_bytes = score_bytes((long)T * B, stretches((long)T * B, V), top);
+  *workspace_bytes = score_bytes((long)T * B, stretches((long)T * B, V, top), top);
   return LSTM_OK;
 }
 
@@ -415,7 +433,7 @@ int lstm_label_score_fwd(int dtype, int T, int B, int V, const void* logits, int
   if (((uintptr_t)logits & (dtype == LSTM_F32 ? 3 : 1)) || (((uintptr_t)label | (uintptr_t)seq_lens | (uintptr_t)logp | (uintptr_t)entropy |
       (uintptr_t)top_logp | (uintptr_t)top_label) & 3) || ((uintptr_t)stats & 7))
     return LSTM_ERR_ALIGN;
-  const int parts = stretches((long)T * B, V);
+  const int parts = stretches((long)T * B, V, top);
   const uint64_t need = score_bytes((long)T * B, parts, top);
   if (need > 0 && !workspace) return LSTM_ERR_NULL;
   if (workspace_bytes < need) return LSTM_ERR_SIZE;

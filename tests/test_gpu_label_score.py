@@ -75,7 +75,7 @@ def _case(T, B, V, seed, spread=3.0):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("T,B,V", [(1, 1, 1), (3, 2, 2), (2, 5, 63), (4, 3, 64), (1, 7, 255), (2, 2, 1000), (3, 3, 4099), (1, 5, 20000), (2, 2, 33001)])
+@pytest.mark.parametrize("T,B,V", [(1, 1, 1), (3, 2, 2), (2, 5, 63), (4, 3, 64), (1, 7, 255), (2, 2, 1000), (3, 3, 4099), (1, 5, 20000), (1, 3, 12001), (1, 2, 32768), (1, 257, 5000), (2, 2, 33001)])
 def test_scores_and_gradients(T, B, V, dt):
     rng, x, label = _case(T, B, V, T + V)
     label.flat[0] = -1
