@@ -314,8 +314,8 @@ int lstm_embed(int B, int n, int V, const int32_t* label, const void* W_trg, con
  * Only cT may overlap an input (c0).  workspace: fwd_workspace_bytes or bwd_workspace_bytes of the query, nothing (NULL) where that is 0; nothing in
  * it has to survive a call.
  * Calls with the same inputs agree bit for bit.
- * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative T or B, n < 1, ld too small, more than 2^31 - 1 rows or states), LSTM_ERR_DIRECTION, LSTM_ERR_UNSUPPORTED
- * (dtype), LSTM_ERR_ALIGN (element alignment), LSTM_ERR_SIZE (reserve or workspace), LSTM_ERR_HIP. */
+ * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative T or B, n < 1, ld too small, T > 2^30, B > 65535, n > 2^27, T B or 3 B n > 2^31 - 1),
+ * LSTM_ERR_DIRECTION, LSTM_ERR_UNSUPPORTED (dtype), LSTM_ERR_ALIGN (element alignment), LSTM_ERR_SIZE (reserve or workspace), LSTM_ERR_HIP. */
 int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* fwd_workspace_bytes, uint64_t* bwd_workspace_bytes);
 int lstm_gated_scan_fwd(int dtype, int direction, int T, int B, int n, const void* z, int64_t ldz, const float* c0, const int32_t* seq_lens,
                         void* y, int64_t ldy, float* cT, void* reserve, uint64_t reserve_bytes, void* workspace, uint64_t workspace_bytes,
@@ -345,8 +345,8 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call; nothing, NULL, where
  *   that is 0); nothing in it has to survive a call.
  * Calls with the same inputs agree bit for bit.
- * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0, 2^23 rows or more), LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN,
- * LSTM_ERR_SIZE, LSTM_ERR_HIP. */
+ * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0, 2^23 rows or more; backward also 2^24 or more stretches of 4096 float or 8192 bfloat16 labels),
+ * LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN, LSTM_ERR_SIZE, LSTM_ERR_HIP. */
 int lstm_label_score_query(int T, int B, int V, int top, uint64_t* workspace_bytes);
 int lstm_label_score_fwd(int dtype, int T, int B, int V, const void* logits, int64_t ld, const int32_t* label, const int32_t* seq_lens,
                          float* logp, float* entropy, float* stats, int top, float* top_logp, int32_t* top_label, void* workspace,
@@ -373,6 +373,7 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
  *   gradient by nothing).  States of zeros (bytes and scales) are the start.  An infinite m or r makes its block of 256 NaN.
  *   lr and step may be in device memory (lr_dev, step_dev: not NULL), so that a captured call follows a schedule; lr and step are then not read
  *   (a step below 1 there counts as 1).
+ *   With eps = 0 an element whose gradients were all 0 is 0 / 0.
  *   The same tensor must not occur twice, nor overlap another.  count may be 0 for a tensor (nothing done) and for the call.
  *   Any element alignment is taken; tensors whose arrays start at multiples of 16 bytes (8-bit states: of 4, bfloat16: of 8) are faster.
  * Both only enqueue work, allocate nothing and give the same bits for the same inputs.

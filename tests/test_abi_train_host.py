@@ -21,7 +21,7 @@ def test_gated_scan_arguments():
     for gone in range(3):
         assert L.lstm_gated_scan_query(4, 2, 8, *[None if i == gone else U() for i in range(3)]) == -1
     assert Bn.gated_scan_query(1, 768, 1000)[1] == 0 and Bn.gated_scan_query(40000, 1, 64)[1] > 0 and Bn.gated_scan_query(4, 2, 8)[2] > 0
-    for T, B, n in ((-1, 2, 8), (4, -1, 8), (4, 2, 0), (4, 70000, 8), (1 << 20, 1 << 15, 8), (4, 1 << 15, 1 << 15)):
+    for T, B, n in ((-1, 2, 8), (4, -1, 8), (4, 2, 0), (4, 70000, 8), (1 << 20, 1 << 15, 8), (4, 1 << 15, 1 << 15), ((1 << 30) + 1, 1, 1), (2 ** 31 - 1, 1, 1), (4, 1, (1 << 27) + 1)):
         assert L.lstm_gated_scan_query(T, B, n, U(), U(), U()) == -2
     base = dict(dt=1, dir=1, T=4, B=2, n=8, z=P, ldz=24, c0=None, lens=None, y=P, ldy=8, cT=None, res=P, rb=1 << 20, ws=P, wb=1 << 20)
     fwd = lambda **o: L.lstm_gated_scan_fwd(*[{**base, **o}[k] for k in base], None)
@@ -40,18 +40,18 @@ def test_gated_scan_arguments():
 
 def test_label_score_arguments():
     q = L.lstm_label_score_query
-    assert _value(q, 1, 12, 20000, 5) > 0 and _value(q, 80, 64, 20000, 0) == 0 and q(1, 2, 10, 0, None) == -1
+    assert _value(q, 1, 12, 100000, 5) > 0 and _value(q, 1, 12, 20000, 5) == 0 and _value(q, 80, 64, 20000, 0) == 0 and q(1, 2, 10, 0, None) == -1
     assert q(-1, 2, 10, 0, U()) == -2 and q(1, -2, 10, 0, U()) == -2 and q(1, 2, 0, 0, U()) == -2 and q(1, 2, 10, -1, U()) == -2 and q(1 << 16, 1 << 16, 10, 0, U()) == -2
     assert q(1, 2, 10, 17, U()) == -4 and q(1, 2, (1 << 26) + 1, 0, U()) == -4
     base = dict(dt=0, T=1, B=2, V=10, x=P, ld=10, label=P, lens=None, logp=P, ent=P, lse=P, top=2, tp=P, tl=P, ws=P, wb=1 << 20)
     fwd = lambda **o: L.lstm_label_score_fwd(*[{**base, **o}[k] for k in base], None)
     base_b = dict(dt=0, T=1, B=2, V=10, x=P, ld=10, label=P, lens=None, lse=P, ent=P, dl=P, de=P, dx=P + 4096, ldd=10)
     bwd = lambda **o: L.lstm_label_score_bwd(*[{**base_b, **o}[k] for k in base_b], None)
-    assert [fwd(**{k: None}) for k in ("x", "label", "tp", "tl")] == [-1] * 4 and fwd(V=20000, ld=20000, ws=None) == -1 and [bwd(**{k: None}) for k in ("x", "label", "lse", "ent", "dx")] == [-1] * 5
+    assert [fwd(**{k: None}) for k in ("x", "label", "tp", "tl")] == [-1] * 4 and fwd(V=100000, ld=100000, ws=None) == -1 and [bwd(**{k: None}) for k in ("x", "label", "lse", "ent", "dx")] == [-1] * 5
     for f in (fwd, bwd):
         assert f(T=-1) == -2 and f(B=-1) == -2 and f(V=0) == -2 and f(ld=9) == -2 and f(dt=2) == -4 and f(V=(1 << 26) + 1) == -4
         assert f(x=P + 2) == -5 and f(lse=P + 4) == -5 and f(lens=P + 1) == -5 and f(T=0) == 0 and f(B=0) == 0
-    assert fwd(top=17) == -4 and fwd(top=-1) == -2 and fwd(V=20000, ld=20000, wb=8) == -6 and bwd(ldd=9) == -2 and bwd(dx=P, ldd=11) == -4 and bwd(de=P + 1) == -5
+    assert fwd(top=17) == -4 and fwd(top=-1) == -2 and fwd(V=100000, ld=100000, wb=8) == -6 and bwd(ldd=9) == -2 and bwd(dx=P, ldd=11) == -4 and bwd(de=P + 1) == -5
     if not GPU:
         assert fwd() == -7 and bwd() == -7 and fwd(top=0, tp=None, tl=None, label=None, logp=None) == -7 and bwd(dl=None, label=None, dx=P) == -7
 

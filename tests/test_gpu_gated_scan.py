@@ -186,6 +186,23 @@ def test_scan_saturated_gates_and_large_values():
     assert torch.equal(h[:, 0, other], f["y"][:, 0, other])
 
 
+@pytest.mark.parametrize("size", [1e-1, 1e-3, 1e-6])
+def test_scan_keeps_the_digits_of_small_values(size):
+    """States of positive candidates of one size, in float storage: no sum cancels, so every state keeps its digits.  A gate is off by (|z_f| + 8) 2^-24 of itself (and
+    of 1 - f), |z_f| <= 2 here; a candidate by 8 2^-24 of itself: of 2^-23 where tanh is at least 1/4, otherwise by the series' eight roundings.  Each is made
+    once a frame and remembered over all T of them at most: (10 + 10 + 8 + 2) T 2^-24, and y 12 2^-24 more."""
+    T, B, n = 60, 3, 130
+    rng = np.random.default_rng(5)
+    z = np.clip(rng.standard_normal((T, B, 3 * n)), -2, 2).astype(np.float32)
+    z[:, :, n:2 * n] = (rng.uniform(0.2, 4, (T, B, n)) * size).astype(np.float32)
+    y, c, _ = R.gated_scan_fwd(z)
+    f = Bn.gated_scan_fwd(dev(z, "f32"))
+    for got, ref in ((host(f["y"]), y), (host(f["cT"]), c)):
+        assert (np.abs(got - ref) <= (30 * T + 12) * 2.0 ** -24 * np.abs(ref)).all(), float((np.abs(got - ref) / np.abs(ref)).max())
+    one = Bn.gated_scan_fwd(dev(z[:1], "f32"), save=False)
+    assert (np.abs(host(one["y"]) - y[:1]) <= 42 * 2.0 ** -24 * np.abs(y[:1])).all()
+
+
 @pytest.mark.parametrize("T,B,n", [(300, 2, 256), (3000, 2, 64), (500, 130, 64)])
 def test_scan_repeats_its_bits_on_any_stream_and_in_a_graph(T, B, n):
     z, dy, c0, dcT, L = _inputs(T, B, n, "bf16", 4, "ragged")
