@@ -253,8 +253,8 @@ __device__ __forceinline__ void update(Block<EIGHT>& x, const AdamArgs::Item& it
     const float g = x.g[k] * gs;
     x.m[k] = x.m[k] * a.b1 + g * a.nb1;
     x.v[k] = x.v[k] * a.b2 + (g * a.nb2) * g;
-    // the quotient by the hardware's reciprocal (1 unit in the last place); the root too where it is not stored
-    root[k] = EIGHT ? sqrtf(x.v[k]) : __builtin_amdgcn_sqrtf(x.v[k]);
+    // the quotient by the hardware's reciprocal (1 unit in the last place), the root in full (the hardware's takes a v below 2^-126 for 0)
+    root[k] = sqrtf(x.v[k]);
     x.w[k] = x.w[k] * keep - (x.m[k] * __builtin_amdgcn_rcpf(root[k] * inv_root2 + a.eps)) * rate;
   }
   if (WIDE) {

@@ -201,6 +201,16 @@ def test_nan_and_infinite_gradients_stay_where_they_are(bits):
     assert torch.isfinite(s["params"][0][rest]).all() and not torch.isfinite(s["params"][0][700])
 
 
+@pytest.mark.parametrize("g", [1e-17, 1e-19, 1e-20])
+def test_first_step_of_tiny_gradients_without_eps(g):
+    """m / sqrt(v) is g / |g| at the first step however small v is: v = 0.001 g^2 is rounded to 2^-149 at the least, its root by half of that relative to v."""
+    w0, sign = torch.ones(300, device="cuda"), torch.where(torch.arange(300, device="cuda") % 2 == 0, 1.0, -1.0)
+    w, m, v = w0.clone(), torch.zeros_like(w0), torch.zeros_like(w0)
+    Bn.adamw_step([w], [sign * g], [m], [v], lr=0.25, step=1, eps=0.0)
+    off = 2.0 ** -149 / (1e-3 * g * g) + 20 * E
+    assert (np.abs(_f64(w) - (1 - 0.25 * _f64(sign))) <= 0.25 * off + 4 * E).all()
+
+
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
 @pytest.mark.parametrize("counts", [[1], [16383, 16384, 16385], [5, 0, 100003, 1, 40000], [3] * 400])
 @pytest.mark.parametrize("shift", [0, 1, 3])
