@@ -1,6 +1,6 @@
 // The update of a model's weights: the global norm of the gradients, and AdamW over many tensors at once with states in 32 or 8 bits.
 //
-// Both are passes over memory.  The tensors' addresses travel in the launch's arguments (kItems of them, further launches take the
+// Both are passes over memory.  The tensors' addresses travel in the launch's arguments (as many as these hold, further launches take the
 // rest), so nothing is copied to the device, a captured call holds its own table and two calls share nothing.
 #include <math.h>
 #include <algorithm>
@@ -18,18 +18,20 @@ constexpr float kTop8 = 448.f;        // the largest e4m3 value
 
 // ---- the norm ---------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-constexpr int kNormItems = 160;
+constexpr int kNormItems = 254;       // (16 bytes each: 217 tensors in one launch)
+constexpr long kNormMost = 1L << 31;  // elements of an item
 struct NormArgs {
-  struct Item { const void* g; long n; unsigned first; int bf16; } item[kNormItems];
+  uint64_t g[kNormItems];             // address, and 1 if the elements are bfloat16
+  unsigned n[kNormItems], first[kNormItems];
   double* part;                       // one per work-group
   int count;
 };
-// the item that tile t belongs to
-template <typename Item> __device__ __forceinline__ int find(const Item* item, int count, unsigned t) {
+// the item that tile t belongs to, from the items' first tiles
+__device__ __forceinline__ int find(const unsigned* first, int count, unsigned t) {
   int i = 0;
   for (int hi = count; hi - i > 1;) {
     const int mid = (i + hi) / 2;
-    if (t >= item[mid].first) i = mid; else hi = mid;
+    if (t >= first[mid]) i = mid; else hi = mid;
   }
   return i;
 }
@@ -82,10 +84,9 @@ __device__ __forceinline__ double squares(const void* g, long begin, long end, b
 template <bool STREAM>
 __global__ __launch_bounds__(256) void grad_norm_kernel(NormArgs a) {
   __shared__ double red[4];
-  const int i = find(a.item, a.count, blockIdx.x);
-  const NormArgs::Item it = a.item[i];
-  const long begin = (long)(blockIdx.x - it.first) * kNormTile, end = min(it.n, begin + kNormTile);
-  const double s = add_all(squares<256, STREAM>(it.g, begin, end, it.bf16, threadIdx.x), red);
+  const int i = find(a.first, a.count, blockIdx.x);
+  const long begin = (long)(blockIdx.x - a.first[i]) * kNormTile, end = min((long)a.n[i], begin + kNormTile);
+  const double s = add_all(squares<256, STREAM>((const void*)(a.g[i] & ~1ull), begin, end, a.g[i] & 1, threadIdx.x), red);
   if (threadIdx.x == 0) a.part[blockIdx.x] = s;
 }
 __global__ __launch_bounds__(1024) void grad_norm_sum_kernel(const double* __restrict__ part, long count, float max_norm, float* __restrict__ out) {
@@ -102,9 +103,9 @@ __global__ __launch_bounds__(1024) void grad_norm_few_kernel(NormArgs a, unsigne
   __shared__ double red[16];
   double s = 0.0;
   for (unsigned t = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); t < tiles; t += 16) {
-    const int i = find(a.item, a.count, t);
-    const long begin = (long)(t - a.item[i].first) * kNormFewTile;
-    s += squares<64, false>(a.item[i].g, begin, min(a.item[i].n, begin + kNormFewTile), a.item[i].bf16, threadIdx.x & 63);
+    const int i = find(a.first, a.count, t);
+    const long begin = (long)(t - a.first[i]) * kNormFewTile;
+    s += squares<64, false>((const void*)(a.g[i] & ~1ull), begin, min((long)a.n[i], begin + kNormFewTile), a.g[i] & 1, threadIdx.x & 63);
   }
   s = add_all<16>(s, red);
   if (threadIdx.x == 0) write_norm(s, max_norm, out);
@@ -113,19 +114,30 @@ __global__ __launch_bounds__(1024) void grad_norm_few_kernel(NormArgs a, unsigne
 // ---- AdamW ------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) bf16_t bf16x4;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
-constexpr int kItems = 54;
+constexpr int kItems = 58;
+constexpr long kMost = 1L << 28;      // elements of an item
 static_assert(kTile == 4 * kBlock, "a work-group has four wavefronts");
+struct Item {
+  void* p; float* w; const void* g; void* m; void* v; float* ms; float* vs;
+  unsigned n; bool p_bf16, g_bf16, wide; float decay;
+};
 struct AdamArgs {
-  struct Item {
-    void* p; float* w; const void* g; void* m; void* v; float* ms; float* vs;
-    unsigned long n : 48, p_bf16 : 1, g_bf16 : 1, wide : 1; float decay; unsigned first;
-  } item[kItems];
+  void* p[kItems]; float* w[kItems]; const void* g[kItems]; void* m[kItems]; void* v[kItems]; float* ms[kItems]; float* vs[kItems];
+  float decay[kItems];
+  unsigned kind[kItems], first[kItems];            // elements * 8 + p_bf16 + 2 g_bf16 + 4 wide
+  __host__ __device__ __forceinline__ void put(int i, const Item& x, unsigned at) {
+    p[i] = x.p; w[i] = x.w; g[i] = x.g; m[i] = x.m; v[i] = x.v; ms[i] = x.ms; vs[i] = x.vs; decay[i] = x.decay; first[i] = at;
+    kind[i] = x.n << 3 | (unsigned)x.p_bf16 | (unsigned)x.g_bf16 << 1 | (unsigned)x.wide << 2;
+  }
+  __device__ __forceinline__ Item get(int i) const {
+    return {p[i], w[i], g[i], m[i], v[i], ms[i], vs[i], kind[i] >> 3, (kind[i] & 1) != 0, (kind[i] & 2) != 0, (kind[i] & 4) != 0, decay[i]};
+  }
   int count, step;
   double lr, beta1, beta2;
   float b1, nb1, b2, nb2, eps, rate, inv_root2;    // beta, 1 - beta; lr / (1 - beta1^t) and 1 / sqrt(1 - beta2^t) unless lr or the step is in device memory
   const float* lr_dev; const int* step_dev; const float* grad_scale;
 };
-static_assert(sizeof(AdamArgs) <= 4096 && sizeof(NormArgs) <= 4096, "arguments of a launch");
+static_assert(sizeof(AdamArgs) <= 4096 && sizeof(NormArgs) + 16 <= 4096, "arguments of a launch");
 
 // beta^t in 64 bits by repeated squaring: the same on the host and on the device
 __host__ __device__ inline double power(double beta, int t) {
@@ -198,7 +210,7 @@ template <bool EIGHT> struct Block {
 };
 // WIDE: every array of the tensor starts at a multiple of four elements' bytes, and the 256 elements are all there; otherwise element by element.
 template <bool EIGHT, bool WIDE>
-__device__ __forceinline__ void fetch(Block<EIGHT>& x, const AdamArgs::Item& it, long block, int lane) {
+__device__ __forceinline__ void fetch(Block<EIGHT>& x, const Item& it, long block, int lane) {
   const long at = block * kBlock + 4 * lane;
   if (WIDE) {
     load4(it.g, it.g_bf16, at, x.g);
@@ -232,7 +244,7 @@ __device__ __forceinline__ void fetch(Block<EIGHT>& x, const AdamArgs::Item& it,
   if (EIGHT) { x.ms = it.ms[block]; x.vs = it.vs[block]; }
 }
 template <bool EIGHT, bool WIDE>
-__device__ __forceinline__ void update(Block<EIGHT>& x, const AdamArgs::Item& it, const AdamArgs& a, long block, int lane, float gs, float keep, float rate,
+__device__ __forceinline__ void update(Block<EIGHT>& x, const Item& it, const AdamArgs& a, long block, int lane, float gs, float keep, float rate,
                                        float inv_root2) {
 #pragma clang fp contract(off)                                            // every product and sum rounded by itself, as the formula is written
   const long at = block * kBlock + 4 * lane;
@@ -308,14 +320,14 @@ template <bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   if (gs - gs != 0.f) return;                                             // NaN or infinite: the step is passed over
-  const int i = find(a.item, a.count, blockIdx.x);
-  const AdamArgs::Item& it = a.item[i];
+  const int i = find(a.first, a.count, blockIdx.x);
+  const Item it = a.get(i);
   const double lr = a.lr_dev ? (double)*a.lr_dev : a.lr;
   float rate = a.rate, inv_root2 = a.inv_root2;
   if (a.lr_dev || a.step_dev) corrections(lr, a.beta1, a.beta2, a.step_dev ? max(*a.step_dev, 1) : a.step, rate, inv_root2);
   const float keep = (float)(1.0 - lr * it.decay);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long block = (long)(blockIdx.x - it.first) * (kTile / kBlock) + wave, n = it.n;
+  const long block = (long)(blockIdx.x - a.first[i]) * (kTile / kBlock) + wave, n = it.n;
   if (block * kBlock >= n) return;
   Block<EIGHT> x;
   if (it.wide && (block + 1) * kBlock <= n) {
@@ -373,8 +385,7 @@ int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, floa
   if ((rc = device_ok())) return rc;
   hipStream_t s = (hipStream_t)stream;
   double* part = (double*)(((uintptr_t)workspace + 255) / 256 * 256);
-  // tensors of more work-groups than a launch may have are cut into pieces of whole tiles
-  constexpr long kMost = (long)kNormTile << 22;
+  // tensors of more elements than an item has are cut into pieces of whole tiles
   NormArgs a;
   a.part = part; a.count = 0;
   unsigned first = 0;
@@ -392,11 +403,12 @@ int lstm_grad_norm(int count, const lstm_adamw_item* items, float max_norm, floa
   };
   const bool few = elements <= kNormFew && count <= kNormItems;
   for (int i = 0; i < count; ++i)
-    for (long at = 0; at < items[i].count; at += kMost) {
+    for (long at = 0; at < items[i].count; at += kNormMost) {
       if (a.count == kNormItems || first >= (1u << 22)) flush();
       const bool bf16 = items[i].grad_dtype == LSTM_BF16_F32STATE;
-      const long n = std::min((long)items[i].count - at, kMost);
-      a.item[a.count++] = {(const char*)items[i].grad + at * (bf16 ? 2 : 4), n, first, bf16};
+      const long n = std::min((long)items[i].count - at, kNormMost);
+      a.g[a.count] = (uint64_t)(uintptr_t)items[i].grad + (uint64_t)at * (bf16 ? 2 : 4) + (bf16 ? 1 : 0);
+      a.n[a.count] = (unsigned)n; a.first[a.count++] = first;
       first += (unsigned)(few ? (n + kNormFewTile - 1) / kNormFewTile : (n + kNormTile - 1) / kNormTile);
     }
   if (few) {
@@ -442,7 +454,6 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
     if (a.count > 0) hipLaunchKernelGGL(eight ? adamw_kernel<true> : adamw_kernel<false>, dim3(first), dim3(256), 0, (hipStream_t)stream, a);
     a.count = 0; first = 0;
   };
-  constexpr long kMost = (long)kTile << 22;
   for (int i = 0; i < count; ++i)
     for (long at = 0; at < items[i].count; at += kMost) {
       if (a.count == kItems || first >= (1u << 22)) flush();
@@ -451,9 +462,10 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
       const long n = std::min((long)it.count - at, kMost), ss = at * (eight ? 1 : 4);
       const bool wide = (((uintptr_t)it.param & (pb ? 7 : 15)) | ((uintptr_t)it.grad & (gb ? 7 : 15)) | ((uintptr_t)it.master & 15) |
                          (((uintptr_t)it.m | (uintptr_t)it.v) & (eight ? 3 : 15))) == 0;
-      a.item[a.count++] = {(char*)it.param + at * (pb ? 2 : 4), it.master ? it.master + at : nullptr, (const char*)it.grad + at * (gb ? 2 : 4),
-                           (char*)it.m + ss, (char*)it.v + ss, eight ? it.m_scale + at / kBlock : nullptr, eight ? it.v_scale + at / kBlock : nullptr,
-                           (unsigned long)n, pb, gb, wide, it.weight_decay, first};
+      const Item x = {(char*)it.param + at * (pb ? 2 : 4), it.master ? it.master + at : nullptr, (const char*)it.grad + at * (gb ? 2 : 4),
+                      (char*)it.m + ss, (char*)it.v + ss, eight ? it.m_scale + at / kBlock : nullptr, eight ? it.v_scale + at / kBlock : nullptr,
+                      (unsigned)n, pb, gb, wide, it.weight_decay};
+      a.put(a.count++, x, first);
       first += (unsigned)((n + kTile - 1) / kTile);
     }
   flush();

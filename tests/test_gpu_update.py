@@ -133,7 +133,7 @@ def test_adamw_of_a_bfloat16_parameter_without_master(bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
-@pytest.mark.parametrize("count", [43, 44, 45, 200])
+@pytest.mark.parametrize("count", [43, 57, 58, 59, 200])
 def test_adamw_of_many_tensors(count, bits):
     rng = np.random.default_rng(count)
     s = _model([int(n) for n in rng.integers(0, 9000, count)], "f32", "f32", bits, count)
@@ -211,8 +211,28 @@ def test_first_step_of_tiny_gradients_without_eps(g):
     assert (np.abs(_f64(w) - (1 - 0.25 * _f64(sign))) <= 0.25 * off + 4 * E).all()
 
 
+def test_a_tensor_of_more_elements_than_a_table_entry():
+    """Behind 2^28 elements (2^31 for the norm) a tensor goes on in the table's next entry: the elements around there fare as they do in a tensor of their own."""
+    n, cut = (1 << 28) + 300, (1 << 28) - 512
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    p = torch.rand(n, generator=gen, device="cuda").to(torch.bfloat16)
+    g = torch.rand(n, generator=gen, device="cuda").to(torch.bfloat16)
+    st = Bn.adamw_state([p], 8)
+    q, h = p[cut:].clone(), g[cut:].clone()
+    own = Bn.adamw_state([q], 8)
+    for step in (1, 2):
+        Bn.adamw_step([p], [g], lr=1e-2, step=step, **st)
+        Bn.adamw_step([q], [h], lr=1e-2, step=step, **own)
+    assert torch.equal(p[cut:], q) and not torch.equal(g[cut:], q)
+    for k in ("m", "v"):
+        assert torch.equal(st[k][0][cut:].view(torch.uint8), own[k][0].view(torch.uint8)) and torch.equal(st[k + "_scale"][0][cut // 256:], own[k + "_scale"][0])
+    del p, g, st
+    ones = torch.ones((1 << 31) + 5, dtype=torch.bfloat16, device="cuda")
+    assert float(Bn.grad_norm([ones])[0]) == float(np.float32(math.sqrt((1 << 31) + 5)))
+
+
 @pytest.mark.parametrize("grad", ["f32", "bf16"])
-@pytest.mark.parametrize("counts", [[1], [16383, 16384, 16385], [5, 0, 100003, 1, 40000], [3] * 400])
+@pytest.mark.parametrize("counts", [[1], [16383, 16384, 16385], [5, 0, 100003, 1, 40000], [3] * 400, [300] * 255])
 @pytest.mark.parametrize("shift", [0, 1, 3])
 def test_grad_norm(counts, grad, shift):
     s = _model(counts, "f32", grad, 32, len(counts), shift)
