@@ -535,7 +535,10 @@ uint64_t reserve_need(int T, int B, int n) { return (uint64_t)cdiv(T, seg_of(T))
 // backward pass).
 struct Cut { int V, waves, parts, per; };
 Cut cut_of(int T, int B, int n, int V) {
-  if (T > 1 && (long)cdiv(n, 128) * B < 256) V = 1;                       // twice the work-groups: 2048 frames of 16 rows of 1024 87 -> 69 us forward, 147 -> 109 backward
+  // Single values instead of words where these give few work-groups: 2048 frames of 16 rows of 1024 87 -> 69 us forward, 147 -> 109 backward; 2048 of 2 rows of 512
+  // 22 -> 16 and 29 -> 21.  Not where time is cut either way and long enough to be cut as often as one likes (16384 of 8 rows of 1024 336 and 559 against 322 and 514).
+  const long wide_groups = (long)cdiv(n, 128) * B;
+  if (T > 1 && wide_groups < 256 && !(T >= 16384 && wide_groups <= 64)) V = 1;
   Cut c = {V, std::max(1, std::min(kWaves, cdiv(T, seg_of(T)))), 1, std::max(T, 1)};
   const long groups = (long)cdiv(n, 64 * V) * B;
   constexpr long kGroups = 512;

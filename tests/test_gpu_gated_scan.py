@@ -79,7 +79,7 @@ def test_scan_shapes(T, B, n, dt, direction):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("T,B,n,direction", [(3000, 1, 96, 1), (5001, 1, 130, -1), (2049, 2, 258, 1), (1030, 3, 64, -1)])
+@pytest.mark.parametrize("T,B,n,direction", [(3000, 1, 96, 1), (5001, 1, 130, -1), (2049, 2, 258, 1), (1030, 3, 64, -1), (16500, 1, 130, -1)])
 def test_scan_long(T, B, n, direction, dt):
     _compare(T, B, n, dt, direction, None, seed=7)
     _compare(T, B, n, dt, direction, "ragged", seed=8)
