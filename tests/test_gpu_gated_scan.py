@@ -227,6 +227,31 @@ def test_scan_repeats_its_bits_on_any_stream_and_in_a_graph(T, B, n):
     assert all(torch.equal(a, b) for a, b in zip(first, second)) and all(torch.equal(a, b) for a, b in zip(first, run()))
 
 
+def test_scan_behind_32_bit_offsets():
+    """The last rows of 4.3e9 pre-activations have the bits of a call of their own; the last frames of a text of 2.4e9 those of one that begins 3000 frames before
+    the end, up to what compositions round: with f <= sigmoid(1) nothing is left of a state after that, and a frame's roundings add up to 20 2^-24 / (1 - f) of the largest."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *shape: torch.empty(*shape, dtype=torch.bfloat16, device="cuda").uniform_(-1, 1, generator=gen)
+    z, dy = rnd(3, 60000, 24000), rnd(3, 60000, 8000)
+    f = Bn.gated_scan_fwd(z)
+    g = Bn.gated_scan_bwd(f, z, dy, want_db=False)
+    own = Bn.gated_scan_fwd(z[:, -2:].contiguous())
+    own_g = Bn.gated_scan_bwd(own, z[:, -2:].contiguous(), dy[:, -2:].contiguous(), want_db=False)
+    assert torch.equal(f["y"][:, -2:], own["y"]) and torch.equal(f["cT"][-2:], own["cT"])
+    assert torch.equal(g["dz"][:, -2:], own_g["dz"]) and torch.equal(g["dc0"][-2:], own_g["dc0"])
+    del z, dy, f, g
+    z, dy = rnd(800000, 1, 3000), rnd(800000, 1, 1000)
+    f = Bn.gated_scan_fwd(z)
+    g = Bn.gated_scan_bwd(f, z, dy)
+    own = Bn.gated_scan_fwd(z[-3000:])
+    own_g = Bn.gated_scan_bwd(own, z[-3000:], dy[-3000:])
+    tol = 20 * 2.0 ** -24 / (1 - 0.7311)
+    assert ((f["cT"] - own["cT"]).abs() <= tol).all()
+    for a, b, most in ((f["y"], own["y"], 1.0), (g["dz"], own_g["dz"], 4.0)):
+        a, b = a[-1000:].float(), b[-1000:].float()
+        assert ((a - b).abs() <= 2.0 ** -7 * b.abs() + most * tol).all()             # (two roundings to bfloat16)
+
+
 def test_scan_refuses_what_it_cannot_take():
     z = torch.zeros(4, 2, 24, device="cuda")
     with pytest.raises(AssertionError):

@@ -232,6 +232,26 @@ def test_repeats_its_bits_on_any_stream_and_in_a_graph():
     assert all(torch.equal(a, b) for a, b in zip(first, second)) and all(torch.equal(a, b) for a, b in zip(first, run()))
 
 
+def test_rows_behind_32_bit_offsets():
+    """The last rows of 2.4e9 logits against a call of their own, whose sums are put together differently: 60001 terms in float, a few hundred a
+    lane and then lane by lane, under 500 2^-24 of the sum (of the entropy's, |x - m| <= 40 times that); a gradient is a product with p and is rounded once on either side."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.empty(40000, 60001, dtype=torch.bfloat16, device="cuda").normal_(0, 3, generator=gen)
+    label = torch.randint(0, 60001, (40000,), generator=gen, device="cuda", dtype=torch.int32)
+    w = torch.rand(40000, generator=gen, device="cuda")
+    f = Bn.label_score_fwd(x, label, top=4)
+    d = Bn.label_score_bwd(f, x, label, w, w)
+    own = Bn.label_score_fwd(x[-3:], label[-3:], top=4)
+    own_d = Bn.label_score_bwd(own, x[-3:], label[-3:], w[-3:], w[-3:])
+    assert torch.equal(f["top_label"][-3:], own["top_label"]) and torch.equal(f["stats"][-3:, 0], own["stats"][:, 0])
+    tol = 500 * 2.0 ** -24
+    for k in ("logp", "top_logp"):
+        assert ((f[k][-3:] - own[k]).abs() <= tol + 2.0 ** -22 * own[k].abs()).all(), k
+    assert ((f["entropy"][-3:] - own["entropy"]).abs() <= 40 * tol).all()
+    assert ((d[-3:].float() - own_d.float()).abs() <= (2.0 ** -7 + 100 * tol) * own_d.float().abs() + 1e-30).all()
+    assert torch.equal(d[-3:] == 0, own_d == 0)
+
+
 def test_refusals():
     x, l = torch.zeros(2, 3, 10, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
     bad = AssertionError
