@@ -27,6 +27,7 @@ inline int seg_of(int T) { return T <= kShort ? kSegShort : kSeg; }
 // what lies outside (a lane behind the last unit, a frame that is not there) is read as 0 and not written, without a branch.
 typedef __amdgpu_buffer_rsrc_t Row;
 constexpr unsigned kOutside = 0x80000000u;
+constexpr int kLine = 128;              // bytes of a line of the L2 cache
 constexpr int kNonTemporal = 2;         // cache policy of a load: past the caches
 template <typename T, int V> struct Word;
 template <> struct Word<float, 1> {
@@ -91,6 +92,7 @@ struct ScanArgs {
   float2* join;                       // [parts][B][n]: what a part's frames do to a state, (factor, addend)
   float* first;                       // [B][n]: copy of c0 or dcT
   int T, B, n, direction;
+  bool shared;                        // columns of a row share lines of 128 bytes
   int parts, per;                     // time is cut into parts of `per` valid frames (a multiple of a work-group's round)
 };
 __device__ __forceinline__ int valid_frames(const int* lens, int b, int T) {
@@ -122,6 +124,26 @@ template <typename T> struct Rows {
 template <typename T> __device__ __forceinline__ Row row_at(const void* base, long row, long ld, int columns) {
   return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)base + row * ld * (long)sizeof(T)), 0, columns * (int)sizeof(T), kBufFlags);
 }
+
+// Which columns (in work-groups), row of the batch and part a work-group takes.  Work-groups go to the eight XCDs in turn; all columns of a row go to one of them, so that
+// the lines where one work-group's units end and the next one's begin meet in its L2 instead of being read, and written in pieces, by two (with the note on non-temporal loads below:
+// 2000 frames of 32 rows of 1000 bfloat16 values 130 -> 118 us forward, 311 -> 226 backward; 1024, whose lines are nobody else's, 112 and 202 without it, 113 and 209 with it).
+struct Place {
+  int x, b, part;
+  __device__ __forceinline__ explicit Place(bool shared) {
+    unsigned row = blockIdx.y + gridDim.y * blockIdx.z, column = blockIdx.x;
+    if (shared && row < ((gridDim.y * gridDim.z) & ~7u)) {
+      const unsigned id = column + gridDim.x * row, turn = id >> 3;
+      row = turn / gridDim.x;
+      column = turn - row * gridDim.x;
+      row = row * 8 + (id & 7);
+    }
+    row = __builtin_amdgcn_readfirstlane(row);
+    x = __builtin_amdgcn_readfirstlane(column);
+    part = __builtin_amdgcn_readfirstlane(row / gridDim.y);
+    b = (int)row - part * (int)gridDim.y;
+  }
+};
 
 // What a work-group's wavefronts tell each other: the composition of their frames, c -> A c + C, for every unit; two sets, so that one
 // barrier a round is enough.
@@ -155,9 +177,10 @@ template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
-  const int b = blockIdx.y, part = a.parts - 1 - (int)blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place place(a.shared);
+  const int b = place.b, part = a.parts - 1 - place.part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = (int)blockDim.x >> 6;
-  const int u = (blockIdx.x * 64 + lane) * V;
+  const int u = (place.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
   const unsigned o0 = live ? at * (unsigned)sizeof(T) : kOutside, o1 = o0 + a.n * (unsigned)sizeof(T), o2 = o1 + a.n * (unsigned)sizeof(T);
@@ -270,8 +293,9 @@ template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
-  const int b = blockIdx.y, part = blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int u = (blockIdx.x * 64 + lane) * V;
+  const Place place(a.shared);
+  const int b = place.b, part = place.part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = (place.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
   const unsigned o0 = live ? at * (unsigned)sizeof(T) : kOutside, o1 = o0 + a.n * (unsigned)sizeof(T), o2 = o1 + a.n * (unsigned)sizeof(T);
@@ -328,9 +352,10 @@ template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ union { Chain<V, NW> chain; double sum[NW][3][V][64]; } sh;
-  const int b = blockIdx.y, part = a.parts - 1 - (int)blockIdx.z, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place place(a.shared);
+  const int b = place.b, part = a.parts - 1 - place.part, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nw = (int)blockDim.x >> 6;
-  const int u = (blockIdx.x * 64 + lane) * V;
+  const int u = (place.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
   const unsigned o0 = live ? at * (unsigned)sizeof(T) : kOutside, o1 = o0 + a.n * (unsigned)sizeof(T), o2 = o1 + a.n * (unsigned)sizeof(T);
@@ -447,8 +472,9 @@ template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_bwd_join_kernel(ScanArgs a) {
   typedef Word<T, V> W;
   __shared__ Chain<V, NW> chain;
-  const int b = blockIdx.y, part = blockIdx.z + 1, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int u = (blockIdx.x * 64 + lane) * V;
+  const Place place(a.shared);
+  const int b = place.b, part = place.part + 1, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int u = (place.x * 64 + lane) * V;
   const bool live = u < a.n;
   const int at = live ? u : 0;
   const unsigned o0 = live ? at * (unsigned)sizeof(T) : kOutside, o1 = o0 + a.n * (unsigned)sizeof(T), o2 = o1 + a.n * (unsigned)sizeof(T);
@@ -516,13 +542,12 @@ __global__ __launch_bounds__(64 * kDbWaves) void scan_db_kernel(const float* __r
   db[i] = (float)s;
 }
 
-// Whole words of two values?
-bool words(int n, std::initializer_list<long> ld, std::initializer_list<const void*> p) {
-  uintptr_t at = 0;
-  long all = n;
-  for (long l : ld) all |= l;
-  for (const void* q : p) at |= (uintptr_t)q;
-  return (all & 1) == 0 && (at & 3) == 0;
+// Does every gate of every row start at a multiple of `bytes`?
+bool starts_at(uintptr_t bytes, int size, int n, std::initializer_list<long> ld, std::initializer_list<const void*> p) {
+  uintptr_t all = (uintptr_t)n * size;
+  for (long l : ld) all |= (uintptr_t)l * size;
+  for (const void* q : p) all |= (uintptr_t)q;
+  return all % bytes == 0;
 }
 
 int scan_dims(int T, int B, int n) {
@@ -581,7 +606,8 @@ void place(ScanArgs& a, const Cut& c, void* workspace, bool backward) {
 int status() { return hipGetLastError() == hipSuccess ? LSTM_OK : LSTM_ERR_HIP; }
 
 // STREAM: a call that moves more than the last-level cache holds (us, 32768 x 1 x 1024 float 167 -> 153 forward and 275 -> 261 backward, 512 x 64 x 2048 bfloat16 121 -> 110
-// forward, 1500 x 32 x 1024 141 -> 125 backward; 80 x 64 x 1000, which fits, 19 -> 23 backward).
+// forward, 1500 x 32 x 1024 141 -> 125 backward; 80 x 64 x 1000, which fits, 19 -> 23 backward), of rows whose work-groups share no lines: those are to stay in L2 for the
+// neighbour (2000 x 32 x 1000 bfloat16 120 -> 118 forward, 276 -> 226 backward without it).
 template <typename T, int V, bool STREAM>
 int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
   const dim3 grid(cdiv(a.n, 64 * V), a.B, c.parts), most(grid.x, grid.y, c.parts - 1);
@@ -608,7 +634,7 @@ int run_bwd(const ScanArgs& a, const Cut& c, float* db, hipStream_t s) {
   if (db) hipLaunchKernelGGL(scan_db_kernel, dim3(cdiv(3L * a.n, 64)), dim3(64 * kDbWaves), 0, s, a.dbpart, db, c.parts * a.B, 3 * a.n);
   return status();
 }
-bool streams(const ScanArgs& a, int size, int values) { return (uint64_t)a.T * a.B * a.n * size * values > kLastLevelBytes; }      // values: a unit's, of a frame
+bool streams(const ScanArgs& a, int size, int values) { return !a.shared && (uint64_t)a.T * a.B * a.n * size * values > kLastLevelBytes; }      // values: a unit's, of a frame
 template <typename T, int V>
 int run_fwd(const ScanArgs& a, const Cut& c, hipStream_t s) {
   if (a.T <= 1) {
@@ -656,7 +682,9 @@ int lstm_gated_scan_fwd(int dtype, int direction, int T, int B, int n, const voi
   ScanArgs a = {};
   a.z = z; a.ldz = ldz; a.c0 = c0; a.lens = seq_lens; a.y = y; a.ldy = ldy; a.cT = cT; a.kept = reserve ? aligned((float*)reserve) : nullptr;
   a.T = T; a.B = B; a.n = n; a.direction = direction;
-  const Cut c = cut_of(T, B, n, dtype == LSTM_BF16_F32STATE && words(n, {ldz, ldy}, {z, y}) ? 2 : 1);
+  const int size = dtype == LSTM_F32 ? 4 : 2;
+  a.shared = !starts_at(kLine, size, n, {ldz, ldy}, {z, y});
+  const Cut c = cut_of(T, B, n, size == 2 && starts_at(4, size, n, {ldz, ldy}, {z, y}) ? 2 : 1);
   place(a, c, workspace, false);
   return dtype == LSTM_F32 ? run_fwd<float, 1>(a, c, (hipStream_t)stream) : c.V == 2 ? run_fwd<bf16_t, 2>(a, c, (hipStream_t)stream) : run_fwd<bf16_t, 1>(a, c, (hipStream_t)stream);
 }
@@ -680,7 +708,9 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
   ScanArgs a = {};
   a.z = z; a.ldz = ldz; a.lens = seq_lens; a.kept = (float*)aligned((const float*)reserve); a.dy = dy; a.lddy = lddy; a.dcT = dcT; a.dz = dz; a.lddz = lddz;
   a.dc0 = dc0; a.T = T; a.B = B; a.n = n; a.direction = direction;
-  const Cut c = cut_of(T, B, n, dtype == LSTM_BF16_F32STATE && words(n, {ldz, lddy, lddz}, {z, dy, dz}) ? 2 : 1);
+  const int size = dtype == LSTM_F32 ? 4 : 2;
+  a.shared = !starts_at(kLine, size, n, {ldz, lddy, lddz}, {z, dy, dz});
+  const Cut c = cut_of(T, B, n, size == 2 && starts_at(4, size, n, {ldz, lddy, lddz}, {z, dy, dz}) ? 2 : 1);
   place(a, c, workspace, true);
   if (!db) a.dbpart = nullptr;
   return dtype == LSTM_F32 ? run_bwd<float, 1>(a, c, db, s) : c.V == 2 ? run_bwd<bf16_t, 2>(a, c, db, s) : run_bwd<bf16_t, 1>(a, c, db, s);
