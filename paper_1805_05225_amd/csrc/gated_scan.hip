@@ -172,7 +172,7 @@ __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wav
 // A work-group takes 64 V units of one row of the batch through a part of time, NW * SEG frames a round: every wavefront has SEG of them in
 // registers, composes them into one step c -> A c + C, gets the state that enters them from the others' compositions and walks them
 // with it.  So all loads of a round are in flight together, z is read once and only the compositions cross wavefronts.  80 frames of 64 rows of 1000 bfloat16 values, lengths
-// 20 to 80: 13 us, one round, latency; 1500 of 32 rows of 1024, lengths 200 to 1500: 83 (264 MB), the longest rows' work-groups; 32768 of one row of 1024 float: 107 (537 MB), memory.
+// 20 to 80: 12 us, a round or two, latency; 1500 of 32 rows of 1024, lengths 200 to 1500: 83 (264 MB), the longest rows' work-groups; 32768 of one row of 1024 float: 107 (537 MB), memory.
 template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a)
 }
 
 // The same from the other end.  A wavefront works its SEG states out again from the one that the forward pass kept in front of them; what
-// passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.  The calls above: 17, 125 (519 MB) and 196 us (940 MB).
+// passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.  The calls above: 16, 125 (519 MB) and 196 us (940 MB).
 template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
