@@ -61,11 +61,12 @@ template <typename T, int V> __device__ __forceinline__ unsigned word_at(const v
 }
 
 // sigmoid(x) and 1 - sigmoid(x) with e = exp(-x): 1 / (1 + e) and e / (1 + e), each with a float's relative accuracy (1 - f has few bits left
-// where a forget gate is near 1).  Where e is infinite the second is inf * 0 and becomes 1; a NaN stays in the first.
+// where a forget gate is near 1) down to 2^-126, below which the hardware's reciprocal and exponential give 0.  The reciprocal does so where e, still finite or not, is above
+// 2^126 (x < -87.33), and e / (1 + e) is 1 there.  A NaN stays in both.
 __device__ __forceinline__ void sigmoid_pair(float x, float& s, float& not_s) {
   const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * x);
   s = __builtin_amdgcn_rcpf(1.f + e);
-  not_s = fminf(e * s, 1.f);
+  not_s = e >= 0x1p126f ? 1.f : e * s;
 }
 __device__ __forceinline__ float sigmoid_(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * x)); }
 // tanh(x) = 1 - 2 / (1 + exp(2 x)) is off by up to 2^-23 of 1, so it keeps few digits of a small value.  In float storage the Taylor series takes its place near 0 (the

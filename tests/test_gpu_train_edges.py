@@ -1,0 +1,78 @@
+"""GPU parity of the gated scan, the label scores and the update where a value, a size or an address lies at the edge of what a formula's arithmetic can hold
+or a rule decides, against oracle/train_oracle.py and against the formula carried out rounding by rounding."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from oracle import train_oracle as R
+from tests.gpu_util import dev, host, tdtype
+
+Bn = None
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _binding():
+    global Bn
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_1805_05225_amd import binding
+    Bn = binding
+    yield
+
+
+# ------------------------------------------------------------------------------------------------ gated scan
+
+# every half from -95 to 95, and eighths where exp(-z) or the sigmoid leaves a float's normal range (|z| near 87.3 and 88.7)
+FORGET = np.concatenate([np.arange(-190, 191) / 2.0, np.arange(86 * 8, 90 * 8 + 1) / 8.0, -np.arange(86 * 8, 90 * 8 + 1) / 8.0])
+
+
+def _near(name, got, ref, dt):
+    got = host(got)
+    tol = 1e-4 * np.abs(ref).max() + (2.0 ** -8 * np.abs(ref) if dt == "bf16" else 0)
+    assert np.isfinite(got).all() and (np.abs(got - ref) <= tol).all(), (name, float((np.abs(got - ref) / tol).max()), int((np.abs(got - ref) > tol).sum()))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,B", [(1, 1), (1, 2), (20, 2), (20, 80), (200, 1), (300, 2), (1100, 2)])
+def test_scan_forget_gates_over_their_whole_range(T, B, dt):
+    """A forget gate of every size: where f has no room in a float 1 - f is 1, and the candidate and its gradient are whole.  The values of FORGET go round over units and frames, one
+    sign in even frames and the other in odd ones, so that f <= 1/2 in every second frame.
+    Tolerance: a gate is off by at most (|z| + 8) 2^-24 of min(f, 1 - f) < 9 2^-24, candidate, product and sum by 8 2^-24 more; an error is halved every second frame, so a state or a
+    carried gradient is off by less than 2 * 2 * 17 2^-24 = 4.1e-6 of the largest and a value made of three of them by less than 1e-4;
+    db sums T B of those.  bfloat16: half a step, 2^-8, more."""
+    rng = np.random.default_rng(T + B)
+    n = FORGET.size
+    rnd = lambda a: torch.from_numpy(a.astype(np.float32)).to(tdtype(dt)).float().numpy()
+    z, t = rng.standard_normal((T, B, 3 * n)), np.arange(T)[:, None, None]
+    v = np.sort(FORGET)
+    deal = v[(np.arange(n)[None, None, :] + 37 * (t // 2) + 11 * np.arange(B)[None, :, None]) % n]
+    z[:, :, :n] = np.abs(deal) * np.where(deal[:1] > 0, 1.0, -1.0) * np.where(t % 2 == 0, 1.0, -1.0)
+    z, dy = rnd(z), rnd(rng.standard_normal((T, B, n)))
+    c0, dcT = (rng.standard_normal((B, n)).astype(np.float32) for _ in range(2))
+    print("  forget gates T=%d B=%d %s" % (T, B, dt), flush=True)
+    for direction in (1, -1):
+        yo, co, _ = R.gated_scan_fwd(z, c0, None, direction)
+        dzo, dco, dbo = R.gated_scan_bwd(z, dy, c0, None, dcT, direction)
+        f = Bn.gated_scan_fwd(dev(z, dt), dev(c0), direction=direction)
+        g = Bn.gated_scan_bwd(f, dev(z, dt), dev(dy, dt), None, dev(dcT))
+        _near("y", f["y"], yo, dt)
+        _near("cT", f["cT"], co, "f32")
+        _near("dz", g["dz"], dzo, dt)
+        _near("dc0", g["dc0"], dco, "f32")
+        assert (np.abs(host(g["db"]) - dbo) <= T * B * 1e-4 * np.abs(dzo).max()).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_scan_of_a_nan_forget_gate(dt):
+    """It stays in its unit, in all three gates' gradients of its frame and in what is carried on from there."""
+    z = np.zeros((3, 1, 12), dtype=np.float32)
+    z[1, 0, 2] = np.nan
+    for frames in (slice(0, 3), slice(1, 2)):
+        zt = dev(z[frames], dt)
+        f = Bn.gated_scan_fwd(zt, torch.ones(1, 4, device="cuda"))
+        g = Bn.gated_scan_bwd(f, zt, torch.ones_like(f["y"]))
+        at = 1 if zt.shape[0] > 1 else 0
+        unit = [False, False, True, False]
+        assert torch.isnan(f["cT"][0]).tolist() == unit and torch.isnan(f["y"][at, 0]).tolist() == unit
+        assert torch.isnan(g["dz"][at, 0]).tolist() == 3 * unit and torch.isnan(g["dc0"][0]).tolist() == unit and torch.isnan(g["db"]).tolist() == 3 * unit
