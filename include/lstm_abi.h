@@ -313,7 +313,8 @@ int lstm_embed(int B, int n, int V, const int32_t* label, const void* W_trg, con
  * two bfloat16 values (even n, ld and addresses of whole words) are faster.  T == 0 or B == 0 is legal: cT = c0, dc0 = dcT, db = 0.
  * Only cT may overlap an input (c0).  workspace: fwd_workspace_bytes or bwd_workspace_bytes of the query, nothing (NULL) where that is 0; nothing in
  * it has to survive a call.
- * Calls with the same inputs agree bit for bit.
+ * The same call repeats its bits.  So does one on the same values elsewhere in memory, but for bfloat16 texts of 16384 frames and more of few rows: whether all rows
+ * start at whole words decides there how frames are grouped, and so the last bits of float sums.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative T or B, n < 1, ld too small, T > 2^30, B > 65535, n > 2^27, T B or 3 B n > 2^31 - 1),
  * LSTM_ERR_DIRECTION, LSTM_ERR_UNSUPPORTED (dtype), LSTM_ERR_ALIGN (element alignment), LSTM_ERR_SIZE (reserve or workspace), LSTM_ERR_HIP. */
 int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* fwd_workspace_bytes, uint64_t* bwd_workspace_bytes);
@@ -344,7 +345,8 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *   dlogits [T][B][ldd >= V], which may be logits (with ldd = ld).
  *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call; nothing, NULL, where
  *   that is 0); nothing in it has to survive a call.
- * Calls with the same inputs agree bit for bit.
+ * The same call repeats its bits.  A row that lies differently to the 16-byte boundaries, among another number of rows or with another `top` may be summed in
+ * another order: its values then agree to the rounding of float sums.  The alternatives' labels do not depend on any of these.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0, 2^23 rows or more; backward also 2^24 or more stretches of 4096 float or 8192 bfloat16 labels),
  * LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN, LSTM_ERR_SIZE, LSTM_ERR_HIP. */
 int lstm_label_score_query(int T, int B, int V, int top, uint64_t* workspace_bytes);
@@ -376,7 +378,8 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
  *   With eps = 0 an element whose gradients were all 0 is 0 / 0.
  *   The same tensor must not occur twice, nor overlap another.  count may be 0 for a tensor (nothing done) and for the call.
  *   Any element alignment is taken; tensors whose arrays start at multiples of 16 bytes (8-bit states: of 4, bfloat16: of 8) are faster.
- * Both only enqueue work, allocate nothing and give the same bits for the same inputs.
+ * Both only enqueue work and allocate nothing.  The same call repeats its bits; lstm_adamw_step gives them wherever the tensors lie, while the norm's order within a tensor begins
+ * with the elements in front of its first 16-byte boundary.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative counts, step < 1, lr, beta, eps, max_norm out of range: lr, eps >= 0 and 0 <= beta < 1, finite),
  * LSTM_ERR_UNSUPPORTED (dtypes, states, reserved not 0, a master of a float param), LSTM_ERR_ALIGN, LSTM_ERR_SIZE, LSTM_ERR_HIP. */
 typedef enum { LSTM_STATE_F32 = 0, LSTM_STATE_8BIT = 1 } lstm_state_dtype;

@@ -12,7 +12,7 @@
 #include "common.h"
 #include "exchange_dev.h"
 
-#pragma clang fp contract(off)        // products and sums are fused where it says fma, so that the forms of a kernel give the same bits
+#pragma clang fp contract(off)        // products and sums are fused where it says fma, so that the forms of a kernel give the same bits (where time is cut at the same frames)
 
 namespace lstm {
 namespace {
@@ -557,7 +557,9 @@ int scan_dims(int T, int B, int n) {
 }
 uint64_t reserve_need(int T, int B, int n) { return (uint64_t)cdiv(T, seg_of(T)) * B * n * 4 + 256; }
 
-// How the work is cut.  Short batches have work-groups of fewer wavefronts; where rows and units give too few work-groups for the device, time is cut
+// How the work is cut.  (Where time is cut decides how compositions are grouped, and so the last bits of results.  Only for long texts of few rows, below, does that depend on V, and with it on the
+// addresses of rows: 32768 bfloat16 frames of 2 rows of 512 at odd elements, cut as often as those at whole words, take 112 us forward instead of 95 and 163 backward instead of 153.)
+// Short batches have work-groups of fewer wavefronts; where rows and units give too few work-groups for the device, time is cut
 // into parts, whose compositions a launch before works out (a second reading of two thirds of what the forward pass reads, three quarters of the
 // backward pass).
 struct Cut { int V, waves, parts, per; };

@@ -12,7 +12,7 @@
 #include "common.h"
 #include "exchange_dev.h"
 
-#pragma clang fp contract(off)        // products and sums are fused where it says fma, so that the forms of a kernel give the same bits
+#pragma clang fp contract(off)        // products and sums are fused where it says fma; the forms of a kernel differ in the order of their sums alone
 
 namespace lstm {
 namespace {

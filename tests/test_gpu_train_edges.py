@@ -76,3 +76,37 @@ def test_scan_of_a_nan_forget_gate(dt):
         unit = [False, False, True, False]
         assert torch.isnan(f["cT"][0]).tolist() == unit and torch.isnan(f["y"][at, 0]).tolist() == unit
         assert torch.isnan(g["dz"][at, 0]).tolist() == 3 * unit and torch.isnan(g["dc0"][0]).tolist() == unit and torch.isnan(g["db"]).tolist() == 3 * unit
+
+
+@pytest.mark.parametrize("direction", [1, -1])
+def test_scan_of_long_rows_at_odd_elements(direction):
+    """A long text of few rows whose rows start at whole words of two bfloat16 values, and at odd elements, where time is cut less often: either is the definition's, and either repeats its bits.
+    Tolerances as for other scans: |z_f| <= 7, so 1e-4 of the largest magnitude; bfloat16 half a step, 2^-8, more; db sums T B such values."""
+    T, B, n = 16400, 8, 66
+    rng = np.random.default_rng(16)
+    rnd = lambda a: torch.from_numpy(a.astype(np.float32)).bfloat16()
+    z = rng.standard_normal((T, B, 3 * n))
+    z[:, :, :n] = np.clip(z[:, :, :n] * 1.5 + 2, -7, 7)
+    z, dy = rnd(z), rnd(rng.standard_normal((T, B, n)))
+    c0, dcT = (rng.standard_normal((B, n)).astype(np.float32) for _ in range(2))
+    lens = np.array([T, 0, 1, 300, 9000, T - 1, 16384, 513], dtype=np.int32)
+    yo, co, _ = R.gated_scan_fwd(z.float().numpy(), c0, lens, direction)
+    dzo, dco, dbo = R.gated_scan_bwd(z.float().numpy(), dy.float().numpy(), c0, lens, dcT, direction)
+
+    def rows(x, odd):
+        full = torch.full((T, B, x.shape[2] + odd), float("nan"), dtype=x.dtype, device="cuda")
+        full[:, :, odd:] = x.cuda()
+        return full[:, :, odd:]
+
+    def run(z, dy):
+        f = Bn.gated_scan_fwd(z, dev(c0), dev(lens), direction=direction)
+        return [f["y"], f["cT"], *Bn.gated_scan_bwd(f, z, dy, dev(lens), dev(dcT)).values()]
+
+    for za, da in ((0, 0), (1, 1), (0, 1), (1, 0)):
+        print("  long rows, z %d and dy %d elements behind a whole word" % (za, da), flush=True)
+        zt, dyt = rows(z, za), rows(dy, da)
+        got = run(zt, dyt)
+        for name, x, ref, dt in zip(("y", "cT", "dz", "dc0"), got, (yo, co, dzo, dco), ("bf16", "f32", "bf16", "f32")):
+            _near(name, x, ref, dt)
+        assert (np.abs(host(got[4]) - dbo) <= lens.sum() * 1e-4 * np.abs(dzo).max()).all()
+        assert all(torch.equal(x, y) for x, y in zip(got, run(zt, dyt)))
