@@ -333,7 +333,7 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *   A row is valid iff t < seq_lens[b] (NULL: all); a padded row gives logp = entropy = m = log z = 0, no alternatives, dlogits = 0, and its
  *   logits, label and gradients are not used.  Rows without time: T = 1, seq_lens NULL.
  *   A label outside [0, V) stands for "none": logp = 0, and dlogp of that row is not used.  A logit of -inf is a label that cannot occur: p = 0, no alternative,
- *   gradient 0.  Where nothing can occur (all -inf): m = -inf, log z = 0, logp = -inf, entropy = 0, gradient 0.  A NaN or +inf among a row's
+ *   gradient 0 unless it is the given label, whose logp is -inf and whose gradient is dlogp, as above.  Where nothing can occur (all -inf): m = -inf, log z = 0, logp = -inf, entropy = 0, gradient 0.  A NaN or +inf among a row's
  *   logits makes its values and its gradient NaN, and it has no alternatives.  Places without an alternative hold -inf and label 0.
  *   Where dlogp and dent of a row are both 0 (or not given) its gradient is 0 and its logits are not read.
  *   dtype: LSTM_F32 or LSTM_BF16_F32STATE, the type of logits and dlogits; all else is float or int32, all arithmetic float, the values before

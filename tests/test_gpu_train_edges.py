@@ -110,3 +110,23 @@ def test_scan_of_long_rows_at_odd_elements(direction):
             _near(name, x, ref, dt)
         assert (np.abs(host(got[4]) - dbo) <= lens.sum() * 1e-4 * np.abs(dzo).max()).all()
         assert all(torch.equal(x, y) for x, y in zip(got, run(zt, dyt)))
+
+
+# ------------------------------------------------------------------------------------------------ label scores
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [5, 700, 20000])
+def test_gradient_of_a_label_that_cannot_occur(V, dt):
+    """The given label's logit is -inf and others are possible: logp = -inf, p = 0 there, and the gradient is the formula's: dlogp at the label, -dlogp p elsewhere.
+    Tolerance: p is off by 4e-5 of itself (1e-5 of log z, and its exponential), a bfloat16 gradient by half a step more."""
+    x = np.random.default_rng(V).standard_normal((2, 3, V)).astype(np.float32)
+    x[:, :, 1::2] = -np.inf
+    label = np.full((2, 3), 1)
+    label[1] = 2                                                 # (one that can)
+    wl, we = np.full((2, 3), 0.75, np.float32), np.array([[0, 0.5, -0.25]] * 2, np.float32)
+    xt, lt = dev(x, dt), dev(label.astype(np.int32))
+    f = Bn.label_score_fwd(xt, lt)
+    assert (f["logp"][0] == -np.inf).all() and torch.isfinite(f["logp"][1]).all()
+    d, ref = host(Bn.label_score_bwd(f, xt, lt, dev(wl), dev(we))), R.label_score_bwd(host(xt), label, wl, we)
+    assert (d[0, :, 1] == 0.75).all() and (d[:, :, 3::2] == 0).all()
+    assert (np.abs(d - ref) <= (8 * 4e-5 + (2.0 ** -8 if dt == "bf16" else 0)) * np.abs(ref) + 4e-5 * 2.0 ** -8).all()
