@@ -375,7 +375,8 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
  *   gradient by nothing).  States of zeros (bytes and scales) are the start.  An infinite m or r makes its block of 256 NaN.
  *   lr and step may be in device memory (lr_dev, step_dev: not NULL), so that a captured call follows a schedule; lr and step are then not read
  *   (a step below 1 there counts as 1).
- *   With eps = 0 an element whose gradients were all 0 is 0 / 0.
+ *   With eps = 0 an element whose gradients were all 0 is 0 / 0.  v is held in 32 bits: gradients whose (1 - beta2) g^2 is below 2^-150 leave it 0, and eps alone divides m.
+ *   A positive eps is taken as no less than 2^-149, the smallest float.
  *   The same tensor must not occur twice, nor overlap another.  count may be 0 for a tensor (nothing done) and for the call.
  *   Any element alignment is taken; tensors whose arrays start at multiples of 16 bytes (8-bit states: of 4, bfloat16: of 8) are faster.
  * Both only enqueue work and allocate nothing.  The same call repeats its bits; lstm_adamw_step gives them wherever the tensors lie, while the norm's order within a tensor begins

@@ -265,9 +265,11 @@ __device__ __forceinline__ void update(Block<EIGHT>& x, const Item& it, const Ad
     const float g = x.g[k] * gs;
     x.m[k] = x.m[k] * a.b1 + g * a.nb1;
     x.v[k] = x.v[k] * a.b2 + (g * a.nb2) * g;
-    // the quotient by the hardware's reciprocal (1 unit in the last place), the root in full (the hardware's takes a v below 2^-126 for 0)
+    // the quotient by the hardware's reciprocal (1 unit in the last place), the root in full (the hardware's takes a v below 2^-126 for 0).  A denominator below 2^-126, that of
+    // an element without gradients where eps is that small, is moved into the range that the reciprocal has, or 0 / eps were 0 * inf
     root[k] = sqrtf(x.v[k]);
-    x.w[k] = x.w[k] * keep - (x.m[k] * __builtin_amdgcn_rcpf(root[k] * inv_root2 + a.eps)) * rate;
+    const float den = root[k] * inv_root2 + a.eps, up = den < 0x1p-126f ? 0x1p64f : 1.f;
+    x.w[k] = x.w[k] * keep - (x.m[k] * __builtin_amdgcn_rcpf(den * up)) * up * rate;
   }
   if (WIDE) {
     if (it.w) store4(it.w, false, at, x.w);
@@ -447,7 +449,8 @@ int lstm_adamw_step(const lstm_adamw_desc* d, int count, const lstm_adamw_item* 
   AdamArgs a;
   a.count = 0;
   a.step = d->step; a.lr = d->lr; a.beta1 = d->beta1; a.beta2 = d->beta2;
-  a.b1 = (float)d->beta1; a.nb1 = (float)(1.0 - d->beta1); a.b2 = (float)d->beta2; a.nb2 = (float)(1.0 - d->beta2); a.eps = (float)d->eps;
+  a.b1 = (float)d->beta1; a.nb1 = (float)(1.0 - d->beta1); a.b2 = (float)d->beta2; a.nb2 = (float)(1.0 - d->beta2);
+  a.eps = d->eps > 0.0 ? std::max((float)d->eps, 0x1p-149f) : 0.f;           // (a positive eps stays positive)
   a.lr_dev = d->lr_dev; a.step_dev = d->step_dev; a.grad_scale = d->grad_scale;
   a.rate = a.inv_root2 = 1.f;
   if (!a.lr_dev && !a.step_dev) corrections(a.lr, a.beta1, a.beta2, a.step, a.rate, a.inv_root2);

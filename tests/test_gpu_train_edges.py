@@ -200,3 +200,16 @@ def test_8_bit_codes_of_values_between_two(unit):
         assert st["m_scale"][0].item() == unit and st["v_scale"][0].item() == unit
         assert np.array_equal(host(st["m"][0]), want * sign)
         assert np.array_equal(host(st["v"][0]), np.where((want == 0) & (part > 0), 2.0 ** -9, want))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-38, 1e-40, 2.0 ** -149, 1e-50])
+def test_an_eps_of_any_size_keeps_0_divided_by_it_0(bits, eps):
+    """An element without gradients so far has m = v = 0 and 0 / eps = 0: its weight only decays, however small eps is; the others take the first step's full size, lr.
+    Weights are 1 and the decay's product and the step's sum are rounded: 2 2^-24; the step by 12 2^-24 of itself."""
+    n = 700
+    w, g = torch.ones(n, device="cuda"), torch.zeros(n, device="cuda")
+    g[5::7] = 0.01
+    Bn.adamw_step([w], [g], lr=0.125, step=1, eps=eps, weight_decay=0.5, **Bn.adamw_state([w], bits))
+    want = np.where(host(g) != 0, 1 - 0.0625 - 0.125, 1 - 0.0625)
+    assert (np.abs(host(w) - want) <= 4 * 2.0 ** -24).all()
