@@ -283,9 +283,8 @@ __device__ __forceinline__ void update(Block<EIGHT>& x, const Item& it, const Ad
       }
   }
   if (EIGHT) {
-    // (1 / 448 is no float: a product with it would be another scale for every second maximum)
-    const float new_ms = wave_most(fmaxf(fmaxf(fabsf(x.m[0]), fabsf(x.m[1])), fmaxf(fabsf(x.m[2]), fabsf(x.m[3])))) / kTop8;
-    const float new_vs = wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))) / kTop8;
+    const float new_ms = wave_most(fmaxf(fmaxf(fabsf(x.m[0]), fabsf(x.m[1])), fmaxf(fabsf(x.m[2]), fabsf(x.m[3])))) * (1.f / kTop8);
+    const float new_vs = wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))) * (1.f / kTop8);
     const unsigned cm = pack8(x.m, unit_of(new_ms));
     unsigned cv = pack8(root, unit_of(new_vs));
     // a positive root never becomes 0: code 1, 2^-9, is the smallest
