@@ -370,7 +370,7 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
  *   w is `master` where there is one, and `param` is its rounding; otherwise w is `param` itself.
  *   States of LSTM_STATE_F32: m and v are float.  LSTM_STATE_8BIT: m and r = sqrt(v) lie in blocks of 256 elements (the last one of a tensor
  *   may be short) as 8-bit floats of 4 exponent and 3 mantissa bits (e4m3, largest value 448) in units of a float scale per block,
- *   the block's largest magnitude / 448: m[i] stands for m[i] * m_scale[i / 256], v[i] for (v[i] * v_scale[i / 256])^2.  w is updated with m and v
+ *   the block's largest magnitude times the float next to 1 / 448 (its 448th part, but for the last bit): m[i] stands for m[i] * m_scale[i / 256], v[i] for (v[i] * v_scale[i / 256])^2.  w is updated with m and v
  *   as computed, before their rounding (to nearest; a positive r never becomes 0, so no element's next step divides a remembered
  *   gradient by nothing).  States of zeros (bytes and scales) are the start.  An infinite m or r makes its block of 256 NaN.
  *   lr and step may be in device memory (lr_dev, step_dev: not NULL), so that a captured call follows a schedule; lr and step are then not read

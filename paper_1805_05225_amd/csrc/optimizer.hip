@@ -283,6 +283,7 @@ __device__ __forceinline__ void update(Block<EIGHT>& x, const Item& it, const Ad
       }
   }
   if (EIGHT) {
+    // (the product is as good a scale as the quotient by 448, whose last bit differs for every second maximum: codes are worked out from the scale that is kept)
     const float new_ms = wave_most(fmaxf(fmaxf(fabsf(x.m[0]), fabsf(x.m[1])), fmaxf(fabsf(x.m[2]), fabsf(x.m[3])))) * (1.f / kTop8);
     const float new_vs = wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))) * (1.f / kTop8);
     const unsigned cm = pack8(x.m, unit_of(new_ms));

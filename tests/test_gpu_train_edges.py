@@ -134,6 +134,74 @@ def test_gradient_of_a_label_that_cannot_occur(V, dt):
 
 # ------------------------------------------------------------------------------------------------ update
 
+def _states_step(m, ms, v, vs, g, gs, beta1, beta2):
+    """One step of 8-bit states, every product, sum, root and quotient rounded to float as the definition is written: codes' values and scales."""
+    f = np.float32
+    n = g.size
+    spread = lambda s: np.repeat(s, 256)[:n]
+    b1, nb1, b2, nb2 = f(beta1), f(1.0 - beta1), f(beta2), f(1.0 - beta2)
+    old_m, r = m * spread(ms), v * spread(vs)
+    g = g * f(gs)
+    new_m, new_v = old_m * b1 + g * nb1, (r * r) * b2 + (g * nb2) * g
+    root, out = np.sqrt(new_v), []
+    for x, positive in ((new_m, False), (root, True)):
+        most = np.abs(np.pad(x, (0, -n % 256))).reshape(-1, 256).max(1)
+        scale = most * (f(1) / f(448))
+        q = np.divide(x, spread(scale), out=np.zeros_like(x), where=x != 0)
+        assert x.dtype == scale.dtype == q.dtype == np.float32
+        code = R.to8(q)
+        if positive:
+            code = np.where((code == 0) & (x > 0), 2.0 ** -9, code)
+        out += [code, scale]
+    return out
+
+
+def _put(a, dt, shift):
+    full = torch.zeros(a.size + shift, dtype=dt, device="cuda")
+    full[shift:].copy_(torch.from_numpy(np.asarray(a, dtype=np.float32)).to(dt))
+    return full[shift:]
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("n", [1, 255, 256, 5000, 70001])
+def test_8_bit_states_are_the_formulas_code_for_code(n, shift):
+    """Codes and scales exactly: a scale is the block's largest magnitude times the float next to 1 / 448, and a code the nearest to the correctly rounded quotient by it."""
+    rng = np.random.default_rng(n)
+    blocks = -(-n // 256)
+    e8, f32 = torch.float8_e4m3fn, torch.float32
+    m, v = _put(np.clip(rng.standard_normal(n) * 100, -448, 448), e8, shift), _put(np.clip(np.abs(rng.standard_normal(n)) * 100, 2.0 ** -9, 448), e8, shift)
+    ms, vs = _put(rng.uniform(0.1, 1, blocks) * 1e-5, f32, shift), _put(rng.uniform(0.1, 1, blocks) * 1e-4, f32, shift)
+    w = _put(rng.standard_normal(n), f32, shift)
+    for step, (beta1, beta2) in enumerate(((0.9, 0.999), (0.8, 0.95), (0.0, 0.0), (0.9, 0.98))):
+        g = rng.standard_normal(n) * 10.0 ** rng.uniform(-6, 0, n)
+        g = _put(g, f32, shift)
+        cpu = lambda t: t.float().cpu().numpy()
+        want = _states_step(cpu(m), cpu(ms), cpu(v), cpu(vs), cpu(g), 0.625, beta1, beta2)
+        Bn.adamw_step([w], [g], [m], [v], lr=1e-3, step=step + 1, beta1=beta1, beta2=beta2, m_scale=[ms], v_scale=[vs], grad_scale=torch.tensor([0.625], device="cuda"))
+        for name, got, ref in zip(("m", "m_scale", "v", "v_scale"), (m, ms, v, vs), want):
+            got = cpu(got)
+            assert np.array_equal(got, ref.astype(np.float32)), (name, step, int((got != ref).sum()), got[got != ref][:4], ref[got != ref][:4])
+
+
+@pytest.mark.parametrize("unit", [2.0 ** -10, 2.0 ** -30, 2.0 ** 5])
+def test_8_bit_codes_of_values_between_two(unit):
+    """A block whose scale is a power of two (448 times the float next to 1 / 448 is 1), of values that lie on a code, halfway between two, and next to that on either side: to the nearest, halves to the even code.
+    With beta = 0 the states are m = g and r = sqrt(g^2) = |g|."""
+    code = R.values8()
+    half = (code[1:] + code[:-1]) / 2
+    x = np.concatenate([code, half, half * (1 - 2.0 ** -23), half * (1 + 2.0 ** -23)]).astype(np.float32)
+    for at in range(0, x.size, 255):
+        part = np.concatenate([[448.0], x[at:at + 255]]).astype(np.float32) * np.float32(unit)
+        sign = np.where(np.arange(part.size) % 3 == 1, -1, 1).astype(np.float32)
+        p = [torch.zeros(part.size, device="cuda")]
+        st = Bn.adamw_state(p, 8)
+        Bn.adamw_step(p, [dev(part * sign)], lr=0.1, step=1, beta1=0.0, beta2=0.0, **st)
+        want = R.to8(part.astype(np.float64) / unit)
+        assert st["m_scale"][0].item() == unit and st["v_scale"][0].item() == unit
+        assert np.array_equal(host(st["m"][0]), want * sign)
+        assert np.array_equal(host(st["v"][0]), np.where((want == 0) & (part > 0), 2.0 ** -9, want))
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("eps", [2.0 ** -126, 1e-38, 1e-40, 2.0 ** -149, 1e-50])
 def test_an_eps_of_any_size_keeps_0_divided_by_it_0(bits, eps):
