@@ -313,8 +313,8 @@ int lstm_embed(int B, int n, int V, const int32_t* label, const void* W_trg, con
  * two bfloat16 values (even n, ld and addresses of whole words) are faster.  T == 0 or B == 0 is legal: cT = c0, dc0 = dcT, db = 0.
  * Only cT may overlap an input (c0).  workspace: fwd_workspace_bytes or bwd_workspace_bytes of the query, nothing (NULL) where that is 0; nothing in
  * it has to survive a call.
- * The same call repeats its bits.  So does one on the same values elsewhere in memory, but for bfloat16 texts of 16384 frames and more of few rows: whether all rows
- * start at whole words decides there how frames are grouped, and so the last bits of float sums.
+ * The same call repeats its bits.  So does one on the same values elsewhere in memory, but for bfloat16 texts of 16384 frames and more of few rows:
+ * whether all rows start at whole words decides there how frames are grouped, and so the last bits of float sums.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative T or B, n < 1, ld too small, T > 2^30, B > 65535, n > 2^27, T B or 3 B n > 2^31 - 1),
  * LSTM_ERR_DIRECTION, LSTM_ERR_UNSUPPORTED (dtype), LSTM_ERR_ALIGN (element alignment), LSTM_ERR_SIZE (reserve or workspace), LSTM_ERR_HIP. */
 int lstm_gated_scan_query(int T, int B, int n, uint64_t* reserve_bytes, uint64_t* fwd_workspace_bytes, uint64_t* bwd_workspace_bytes);
@@ -332,9 +332,10 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *     dlogits[v] = dlogp * ([v = label] - p[v]) - dent * p[v] * (log p[v] + entropy)
  *   A row is valid iff t < seq_lens[b] (NULL: all); a padded row gives logp = entropy = m = log z = 0, no alternatives, dlogits = 0, and its
  *   logits, label and gradients are not used.  Rows without time: T = 1, seq_lens NULL.
- *   A label outside [0, V) stands for "none": logp = 0, and dlogp of that row is not used.  A logit of -inf is a label that cannot occur: p = 0, no alternative,
- *   gradient 0 unless it is the given label, whose logp is -inf and whose gradient is dlogp, as above.  Where nothing can occur (all -inf): m = -inf, log z = 0, logp = -inf, entropy = 0, gradient 0.  A NaN or +inf among a row's
- *   logits makes its values and its gradient NaN, and it has no alternatives.  Places without an alternative hold -inf and label 0.
+ *   A label outside [0, V) stands for "none": logp = 0, and dlogp of that row is not used.  A logit of -inf is a label that cannot occur: p = 0, no
+ *   alternative, gradient 0 unless it is the given label, whose logp is -inf and whose gradient is dlogp, as above.  Where nothing can occur (all -inf):
+ *   m = -inf, log z = 0, logp = -inf, entropy = 0, gradient 0.  A NaN or +inf among a row's logits makes its values and its gradient NaN, and it has no
+ *   alternatives.  Places without an alternative hold -inf and label 0.
  *   Where dlogp and dent of a row are both 0 (or not given) its gradient is 0 and its logits are not read.
  *   dtype: LSTM_F32 or LSTM_BF16_F32STATE, the type of logits and dlogits; all else is float or int32, all arithmetic float, the values before
  *   their rounding for dlogits.
@@ -345,8 +346,8 @@ int lstm_gated_scan_bwd(int dtype, int direction, int T, int B, int n, const voi
  *   dlogits [T][B][ldd >= V], which may be logits (with ldd = ld).
  *   V <= 2^26; rows may start at any element.  workspace of lstm_label_score_query bytes (forward call; nothing, NULL, where
  *   that is 0); nothing in it has to survive a call.
- * The same call repeats its bits.  A row that lies differently to the 16-byte boundaries, among another number of rows or with another `top` may be summed in
- * another order: its values then agree to the rounding of float sums.  The alternatives' labels do not depend on any of these.
+ * The same call repeats its bits.  A row that lies differently to the 16-byte boundaries, among another number of rows or with another `top` may be
+ * summed in another order: its values then agree to the rounding of float sums.  The alternatives' labels do not depend on any of these.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (sizes, ld, top < 0, 2^23 rows or more; backward also 2^24 or more stretches of 4096 float or 8192 bfloat16 labels),
  * LSTM_ERR_UNSUPPORTED (dtype, top > 16, V > 2^26, dlogits = logits with another ld), LSTM_ERR_ALIGN, LSTM_ERR_SIZE, LSTM_ERR_HIP. */
 int lstm_label_score_query(int T, int B, int V, int top, uint64_t* workspace_bytes);
@@ -360,7 +361,8 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
  * global norm of the gradients that it is clipped by.  `items` is a HOST array, read during the call.
  *
  * lstm_grad_norm: out[0] = sqrt(sum over all tensors of grad^2), summed in 64 bits in a fixed order; out[1] = min(1, max_norm / out[0]), the factor
- *   that clips it to max_norm, or NaN if the norm is not finite.  Only grad, grad_dtype and count of the items are read.
+ *   that clips it to max_norm, or NaN if a gradient is not finite (a norm beyond a float's range is infinity in out[0], its factor still a
+ *   number).  Only grad, grad_dtype and count of the items are read.
  *   max_norm > 0 (infinity: never clipped).  out: float [2] in device memory; workspace of lstm_grad_norm_query bytes.
  *
  * lstm_adamw_step: with g = grad * grad_scale (*grad_scale in device memory, e.g. out + 1 of lstm_grad_norm; NULL: 1) and t the number of this step, from 1,
@@ -370,17 +372,17 @@ int lstm_label_score_bwd(int dtype, int T, int B, int V, const void* logits, int
  *   w is `master` where there is one, and `param` is its rounding; otherwise w is `param` itself.
  *   States of LSTM_STATE_F32: m and v are float.  LSTM_STATE_8BIT: m and r = sqrt(v) lie in blocks of 256 elements (the last one of a tensor
  *   may be short) as 8-bit floats of 4 exponent and 3 mantissa bits (e4m3, largest value 448) in units of a float scale per block,
- *   the block's largest magnitude times the float next to 1 / 448 (its 448th part, but for the last bit): m[i] stands for m[i] * m_scale[i / 256], v[i] for (v[i] * v_scale[i / 256])^2.  w is updated with m and v
- *   as computed, before their rounding (to nearest; a positive r never becomes 0, so no element's next step divides a remembered
- *   gradient by nothing).  States of zeros (bytes and scales) are the start.  An infinite m or r makes its block of 256 NaN.
+ *   the block's largest magnitude times the float next to 1 / 448 (its 448th part, but for the last bit): m[i] stands for
+ *   m[i] * m_scale[i / 256], v[i] for (v[i] * v_scale[i / 256])^2.  w is updated with m and v as computed, before their rounding (to nearest; a
+ *   positive r never becomes 0, so no element's next step divides a remembered gradient by nothing).  States of zeros (bytes and scales) are the start.  An infinite m or r makes its block of 256 NaN.
  *   lr and step may be in device memory (lr_dev, step_dev: not NULL), so that a captured call follows a schedule; lr and step are then not read
  *   (a step below 1 there counts as 1).
- *   With eps = 0 an element whose gradients were all 0 is 0 / 0.  v is held in 32 bits: gradients whose (1 - beta2) g^2 is below 2^-150 leave it 0, and eps alone divides m.
- *   A positive eps is taken as no less than 2^-149, the smallest float.
+ *   With eps = 0 an element whose gradients were all 0 is 0 / 0.  v is held in 32 bits: gradients whose (1 - beta2) g^2 is below 2^-150 leave it 0,
+ *   and eps alone divides m.  A positive eps is taken as no less than 2^-149, the smallest float.
  *   The same tensor must not occur twice, nor overlap another.  count may be 0 for a tensor (nothing done) and for the call.
  *   Any element alignment is taken; tensors whose arrays start at multiples of 16 bytes (8-bit states: of 4, bfloat16: of 8) are faster.
- * Both only enqueue work and allocate nothing.  The same call repeats its bits; lstm_adamw_step gives them wherever the tensors lie, while the norm's order within a tensor begins
- * with the elements in front of its first 16-byte boundary.
+ * Both only enqueue work and allocate nothing.  The same call repeats its bits; lstm_adamw_step gives them wherever the tensors lie, while the order
+ * of the norm's sums goes by a tensor's 16-byte boundaries.
  * Errors: LSTM_ERR_NULL, LSTM_ERR_DIM (negative counts, step < 1, lr, beta, eps, max_norm out of range: lr, eps >= 0 and 0 <= beta < 1, finite),
  * LSTM_ERR_UNSUPPORTED (dtypes, states, reserved not 0, a master of a float param), LSTM_ERR_ALIGN, LSTM_ERR_SIZE, LSTM_ERR_HIP. */
 typedef enum { LSTM_STATE_F32 = 0, LSTM_STATE_8BIT = 1 } lstm_state_dtype;

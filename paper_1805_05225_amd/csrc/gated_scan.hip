@@ -173,7 +173,8 @@ __device__ __forceinline__ void link(Chain<V, NW>& s, int set, int lane, int wav
 // A work-group takes 64 V units of one row of the batch through a part of time, NW * SEG frames a round: every wavefront has SEG of them in
 // registers, composes them into one step c -> A c + C, gets the state that enters them from the others' compositions and walks them
 // with it.  So all loads of a round are in flight together, z is read once and only the compositions cross wavefronts.  80 frames of 64 rows of 1000 bfloat16 values, lengths
-// 20 to 80: 12 us, a round or two, latency; 1500 of 32 rows of 1024, lengths 200 to 1500: 83 (264 MB), the longest rows' work-groups; 32768 of one row of 1024 float: 107 (537 MB), memory.
+// 20 to 80: 12 us, a round or two, latency; 1500 of 32 rows of 1024, lengths 200 to 1500: 83 (264 MB), the longest rows' work-groups; 32768 of one row of 1024 float, with the
+// compositions of its parts: 147 (797 MB, 5.4 TB/s), memory and, before the first round, the parts in front folded one behind the other.  (In replayed graphs, without a profiler.)
 template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, 4) void gated_scan_fwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
@@ -348,7 +349,8 @@ __global__ __launch_bounds__(64 * NW, 4) void gated_scan_join_kernel(ScanArgs a)
 }
 
 // The same from the other end.  A wavefront works its SEG states out again from the one that the forward pass kept in front of them; what
-// passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.  The calls above: 16, 125 (519 MB) and 196 us (940 MB).
+// passes on is e = f dc, whose frames compose like the forward ones: e -> A e + C with A = the product of f.  The calls above, with the sum of db: 19, 128 (519 MB) and
+// 256 us (1330 MB with the compositions, 5.2 TB/s).
 template <typename T, int V, int NW, int SEG, bool STREAM>
 __global__ __launch_bounds__(64 * NW, SEG == kSeg && sizeof(T) == 2 ? 2 : 4) void gated_scan_bwd_kernel(ScanArgs a) {
   typedef Word<T, V> W;
@@ -565,11 +567,15 @@ uint64_t reserve_need(int T, int B, int n) { return (uint64_t)cdiv(T, seg_of(T))
 struct Cut { int V, waves, parts, per; };
 Cut cut_of(int T, int B, int n, int V) {
   // Single values instead of words where these give few work-groups: 2048 frames of 16 rows of 1024 87 -> 69 us forward, 147 -> 109 backward; 2048 of 2 rows of 512
-  // 22 -> 16 and 29 -> 21.  Not where time is cut either way and long enough to be cut as often as one likes (16384 of 8 rows of 1024 336 and 559 against 322 and 514).
+  // 22 -> 16 and 29 -> 21.  Not where time is cut either way and long enough to be cut as often as one likes (words against single values, forward and backward: 16384 of 1, 4 and 8 rows
+  // of 1024 53, 89 and 51, 87; 156, 269 and 172, 296; 311, 520 and 332, 565; 65536 of 1 row 163, 278 and 175, 302, but of 256 units, where the fold of 128 parts counts, 95, 132 and 68, 97;
+  // beside the rule 8192 of 2 rows 47, 88 and 48, 85, of 8 rows 155, 265 and 165, 287, 16384 of 16 rows 666, 1060 and 487, 865).
   const long wide_groups = (long)cdiv(n, 128) * B;
   if (T > 1 && wide_groups < 256 && !(T >= 16384 && wide_groups <= 64)) V = 1;
   Cut c = {V, std::max(1, std::min(kWaves, cdiv(T, seg_of(T)))), 1, std::max(T, 1)};
   const long groups = (long)cdiv(n, 64 * V) * B;
+  // Time is cut up to 128 work-groups, half the compute units: with more the second reading costs more than the idle units (uncut and cut, forward and backward, float rows of 1024:
+  // 4096 of 10 rows 158, 267 and 184, 319; of 16 219, 404 and 265, 482; 8192 of 10 322, 532 and 393, 629; 1024 of 10 44, 69 and 51, 80).
   constexpr long kGroups = 512;
   const int round = kWaves * kSeg;
   if (groups > 0 && groups <= 128 && T >= 4 * round) {

@@ -1,7 +1,7 @@
 // The update of a model's weights: the global norm of the gradients, and AdamW over many tensors at once with states in 32 or 8 bits.
 //
 // Both are passes over memory.  The tensors' addresses travel in the launch's arguments (as many as these hold, further launches take the
-// rest), so nothing is copied to the device, a captured call holds its own table and two calls share nothing.
+// rest), so nothing is copied to the device, the update needs no workspace, a captured call holds its own table and two calls share nothing.
 #include <math.h>
 #include <algorithm>
 
@@ -18,7 +18,7 @@ constexpr float kTop8 = 448.f;        // the largest e4m3 value
 
 // ---- the norm ---------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-constexpr int kNormItems = 254;       // (16 bytes each: 217 tensors in one launch)
+constexpr int kNormItems = 254;       // (16 bytes each: what 4096 bytes of a launch's arguments hold)
 constexpr long kNormMost = 1L << 31;  // elements of an item
 struct NormArgs {
   uint64_t g[kNormItems];             // address, and 1 if the elements are bfloat16
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(1024) void grad_norm_few_kernel(NormArgs a, unsigne
 // ---- AdamW ------------------------------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) bf16_t bf16x4;
 typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
-constexpr int kItems = 58;
+constexpr int kItems = 58;            // (68 bytes each: likewise)
 constexpr long kMost = 1L << 28;      // elements of an item
 static_assert(kTile == 4 * kBlock, "a work-group has four wavefronts");
 struct Item {
